@@ -48,6 +48,7 @@ extern "C" {
 
 #define MQ_F16 0
 #define MQ_BF16 1
+#define MQ_F32 2 /* parameters of the layer norm only */
 
 /* Library version and the last HIP error code seen by a failing call (0 if none). */
 int mq_version(void);
@@ -393,6 +394,68 @@ int mq_bos_aware_kv_proj(const void* ctx, int B, int T, int K, const void* packe
                          const void* w_f16, const void* bos_out, const float* act_scale, const int32_t* act_zp,
                          const void* bias, void* y, int naive_all_rows, float* act_scale_out, int32_t* act_zp_out,
                          void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Microscaled 4-bit floats (MXFP4), layer norm, and their gradients
+ *
+ * A microscaled matrix stands for [rows, K] values: 32 consecutive values of a row are a block of e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives) times 2^(s - 127), s one byte per block, 255 for a block that holds an infinity or a NaN and stands for NaN throughout.
+ * Quantising takes s = max(0, E - 2), E the biased binary32 exponent of the block's largest magnitude; codes round to nearest, ties to the
+ * even code, and magnitudes past 6 units become 6.  K is a multiple of 32; rows may be any number.  The form in memory is the product's own
+ * (256-byte aligned, mq_mx_bytes); mq_mx_pack and mq_mx_unpack convert from and to rows of codes and scales.
+ *
+ * In this section row strides are `long` and any value of at least a row; 16-bit matrices need no alignment beyond their type's.  (Rows that start on
+ * 16-byte boundaries, and N % 8 == 0, are faster.)  A call with M = 0 rows is MQ_OK and writes nothing but zero sums (mq_layer_norm_grad).
+ * Errors beside those named: MQ_ERR_BAD_ARG (null or misaligned pointer, unknown dtype, negative or NaN eps), MQ_ERR_BAD_SHAPE (M < 0, K or C <= 0, K
+ * not a multiple of 32, a stride below the row, K > 2^21, N > 2^22, C > 16384), MQ_ERR_HIP.
+ * ---------------------------------------------------------------------------------------------- */
+
+/* Bytes of a microscaled matrix (rows padded to 32, columns to 64 and their scales to 256); 0 for an unsupported size. */
+size_t mq_mx_bytes(int rows, int K);
+
+/* x [M,K] of dtype -> microscaled matrix.  Weights and activations have the same form. */
+int mq_mx_quantize(const void* x, int M, int K, long ldx, int dtype, void* mx, void* stream);
+
+/* The values that a microscaled matrix stands for, rounded to dtype (bfloat16 holds every one exactly). */
+int mq_mx_dequantize(const void* mx, int M, int K, int dtype, void* y, long ldy, void* stream);
+
+/* Interchange: codes [M, K/2] bytes (value 2i in the low half of byte i), scales [M, K/32] bytes.  Packing clears the codes of blocks with scale 255. */
+int mq_mx_pack(const uint8_t* codes, const uint8_t* scales, int M, int K, void* mx, void* stream);
+int mq_mx_unpack(const void* mx, int M, int K, uint8_t* codes, uint8_t* scales, void* stream);
+
+/* top [K/32]: the largest scale byte below 255 of every column of blocks (0 if none): what mq_mx_linear_grad takes the weights relative to. */
+int mq_mx_column_top(const void* mx, int rows, int K, uint8_t* top, void* stream);
+
+/* Y = mx(X) W^T + bias (+ residual), X [M,K] and Y [M,N] of dtype, W a microscaled matrix [N,K], bias [N] of dtype (nullable), residual [M,N] of
+ * dtype (nullable; may be Y itself).  X is quantised in the call; products and sums are fp32, rounded once.  Y may overlap X. */
+size_t mq_mx_linear_workspace_bytes(int M, int N, int K);
+int mq_mx_linear(const void* x, int M, int K, long ldx, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual,
+                 long ldr, void* ws, size_t ws_bytes, void* stream);
+
+/* The same on activations that are microscaled already (mq_mx_quantize, mq_layer_norm_mx). */
+int mq_mx_linear_codes(const void* a, int M, int K, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual, long ldr,
+                       void* stream);
+
+/* Gradient of mq_mx_linear with respect to X, the quantisation of X passed straight through: dX = dY W, dY [M,N], dX [M,K] of dtype, sums fp32,
+ * rounded once.  top: mq_mx_column_top of W.  Weights below 2^-37 (bfloat16: 2^-128) of the largest of their block column may be taken as zero. */
+int mq_mx_linear_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* stream);
+
+/* Y = (X - mean) rstd weight + bias over the C columns of each row, rstd = 1 / sqrt(variance + eps), variance = mean of squared deviations.  weight,
+ * bias [C] of param_dtype (MQ_F16, MQ_BF16 or MQ_F32), each nullable (1 and 0).  mean, rstd [M]: nullable outputs, for the gradient.  Sums fp32.
+ * Y may be X. */
+int mq_layer_norm(const void* x, int M, int C, long ldx, const void* weight, const void* bias, int param_dtype, float eps, void* y, long ldy, int dtype,
+                  float* mean, float* rstd, void* stream);
+
+/* The same with the output quantised from its fp32 values into a microscaled matrix [M,C] (C % 32 == 0). */
+int mq_layer_norm_mx(const void* x, int M, int C, long ldx, const void* weight, const void* bias, int param_dtype, float eps, void* mx, int dtype,
+                     float* mean, float* rstd, void* stream);
+
+/* Gradient of the layer norm (and, its quantisation passed straight through, of mq_layer_norm_mx): dX (+ residual, the gradient that reaches X past
+ * the norm; nullable, may be dX itself), dweight [C], dbias [C] (fp32, each nullable).  dX may be dY.  The sums over rows are taken in a fixed order. */
+size_t mq_layer_norm_grad_workspace_bytes(int M, int C);
+int mq_layer_norm_grad(const void* dy, long lddy, const void* x, long ldx, int M, int C, const void* weight, int param_dtype, const float* mean,
+                       const float* rstd, const void* residual, long ldr, void* dx, long lddx, int dtype, float* dweight, float* dbias, void* ws,
+                       size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Bit-width allocation (host only: every pointer in this section is a HOST pointer, no GPU is touched, nothing is

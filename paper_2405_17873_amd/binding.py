@@ -5,7 +5,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import Optional
+from typing import Optional, Union
 
 import torch
 
@@ -13,6 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libmixdq.so")
 
 F16, BF16 = 0, 1
+F32 = 2  # parameters of the layer norm
 LAYOUT_CANONICAL, LAYOUT_KERNEL = 0, 1
 
 _ERRORS = {
@@ -27,7 +28,9 @@ EXPORTS = ("mq_version", "mq_last_hip_error", "mq_tune_force_tile", "mq_tune_for
            "mq_qlinear_w4a8", "mq_qlinear_w2a8", "mq_builtin_workspace_bytes", "mq_qlinear_a8_builtin_ws", "mq_a8_row_bytes", "mq_qlinear_a8_geglu", "mq_qlinear_a8_geglu_dynamic_workspace_bytes", "mq_qlinear_a8_geglu_dynamic", "mq_qlinear_w_only_geglu", "mq_qlinear_w_only_geglu_a8", "mq_qlinear_a8_codes", "mq_conv3x3_w_only",
            "mq_conv_tap_sums", "mq_conv3x3_a8_workspace_bytes", "mq_conv3x3_a8",
            "mq_bos_aware_kv_proj_workspace_bytes", "mq_bos_aware_kv_proj", "mq_alloc_solve", "mq_alloc_split_budget",
-           "mq_alloc_search")
+           "mq_alloc_search", "mq_mx_bytes", "mq_mx_quantize", "mq_mx_dequantize", "mq_mx_pack", "mq_mx_unpack", "mq_mx_column_top",
+           "mq_mx_linear_workspace_bytes", "mq_mx_linear", "mq_mx_linear_codes", "mq_mx_linear_grad", "mq_layer_norm", "mq_layer_norm_mx",
+           "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad")
 
 
 class MixdqError(RuntimeError):
@@ -58,7 +61,8 @@ def load():
         if not os.path.exists(_LIB_PATH):
             raise RuntimeError(f"{_LIB_PATH} is missing: run `python -c 'import __graft_entry__ as g; g.build()'`")
         lib = C.CDLL(_LIB_PATH)
-        for name in ("mq_a8_row_bytes", "mq_split_workspace_bytes", "mq_builtin_workspace_bytes", "mq_conv3x3_a8_workspace_bytes", "mq_packed_bytes", "mq_qlinear_a8_workspace_bytes", "mq_qlinear_a8_geglu_dynamic_workspace_bytes", "mq_bos_aware_kv_proj_workspace_bytes"):
+        for name in ("mq_a8_row_bytes", "mq_split_workspace_bytes", "mq_builtin_workspace_bytes", "mq_conv3x3_a8_workspace_bytes", "mq_packed_bytes", "mq_qlinear_a8_workspace_bytes", "mq_qlinear_a8_geglu_dynamic_workspace_bytes", "mq_bos_aware_kv_proj_workspace_bytes",
+                     "mq_mx_bytes", "mq_mx_linear_workspace_bytes", "mq_layer_norm_grad_workspace_bytes"):
             getattr(lib, name).restype = C.c_size_t
         lib.mq_prof_bracket_overhead_us.restype = C.c_double
         _lib = lib
@@ -727,3 +731,220 @@ def alloc_search(sens_content, params_content, sens_quality, params_quality, bit
                                   _np_ptr(out["feasible"]), _np_ptr(out["objectives"]), _np_ptr(out["choice_content"]),
                                   _np_ptr(out["choice_quality"])), "mq_alloc_search")
     return out
+
+
+# ------------------------------------------- microscaled 4-bit floats, layer norm, and their gradients
+#
+# Matrices are [rows, columns] with contiguous rows, which may lie apart.
+
+
+@dataclass
+class MxTensor:
+    """A [rows, K] matrix in microscaled 4-bit floats, in the product's form.  top: for weights whose layer is differentiated."""
+    data: torch.Tensor                  # uint8, mx_bytes(rows, K)
+    rows: int
+    K: int
+    top: Optional[torch.Tensor] = None  # uint8 [K / 32], the largest scale of every column of blocks
+
+    @property
+    def shape(self):
+        return (self.rows, self.K)
+
+
+def _matrix(t: torch.Tensor, rows=None, cols=None, dtype=None) -> torch.Tensor:
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"expected a matrix on the GPU with contiguous rows, got {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"expected [{rows}, {cols}], got {tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
+    return t
+
+
+def _out(t: Optional[torch.Tensor], rows: int, cols: int, dtype, device) -> torch.Tensor:
+    return torch.empty((rows, cols), dtype=dtype, device=device) if t is None else _matrix(t, rows, cols, dtype)
+
+
+def _ld(t: Optional[torch.Tensor]):
+    """Row stride; a single row's stride says nothing."""
+    return C.c_long(0 if t is None else max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1])
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype, device) -> Optional[torch.Tensor]:
+    if t is None:
+        return None
+    if t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous vector of {n} on {device}, got {tuple(t.shape)} on {t.device}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
+    return t
+
+
+def _bytes_of(ws: torch.Tensor):
+    return C.c_size_t(ws.numel() * ws.element_size())
+
+
+def mx_bytes(rows: int, K: int) -> int:
+    return int(load().mq_mx_bytes(rows, K))
+
+
+def _new_mx(rows: int, K: int, device) -> MxTensor:
+    n = mx_bytes(rows, K)
+    if K <= 0 or K % 32:
+        raise ValueError(f"microscaled matrices have a multiple of 32 columns, got {K}")
+    return MxTensor(torch.empty(n, dtype=torch.uint8, device=device), rows, K)
+
+
+def mx_quantize(x: torch.Tensor) -> MxTensor:
+    """[M, K] fp16/bf16 -> MXFP4: blocks of 32 values of a row, e2m1 codes (nearest, ties to even) times a power of two."""
+    M, K = _matrix(x).shape
+    dt = _dtype_code(x)
+    t = _new_mx(M, K, x.device)
+    _check(load().mq_mx_quantize(_ptr(x), M, K, _ld(x), dt, _ptr(t.data), _stream()), "mq_mx_quantize")
+    return t
+
+
+def mx_quantize_weights(w: torch.Tensor) -> MxTensor:
+    """mx_quantize of a weight matrix [N, K], with what mx_linear_grad needs beside it."""
+    return _with_top(mx_quantize(w))
+
+
+def _with_top(t: MxTensor) -> MxTensor:
+    t.top = torch.empty(t.K // 32, dtype=torch.uint8, device=t.data.device)
+    _check(load().mq_mx_column_top(_ptr(t.data), t.rows, t.K, _ptr(t.top), _stream()), "mq_mx_column_top")
+    return t
+
+
+def mx_dequantize(t: MxTensor, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values that `t` stands for, rounded to dtype (bfloat16 holds every one)."""
+    y = _out(out, t.rows, t.K, dtype, t.data.device)
+    _check(load().mq_mx_dequantize(_ptr(t.data), t.rows, t.K, _dtype_code(y), _ptr(y), _ld(y), _stream()), "mq_mx_dequantize")
+    return y
+
+
+def mx_pack(codes: torch.Tensor, scales: torch.Tensor) -> MxTensor:
+    """Interchange form (codes uint8 [M, K/2], value 2i in the low half of byte i; scales uint8 [M, K/32]) -> MxTensor, ready for a weight."""
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+        raise TypeError("codes and scales are uint8")
+    M, K = codes.shape[0], codes.shape[1] * 2
+    t = _new_mx(M, K, codes.device)
+    if not codes.is_cuda or not codes.is_contiguous() or not scales.is_contiguous() or scales.device != codes.device or tuple(scales.shape) != (M, K // 32):
+        raise ValueError(f"expected contiguous codes [M, K/2] and scales [M, K/32] on the GPU, got {tuple(codes.shape)} and {tuple(scales.shape)}")
+    _check(load().mq_mx_pack(_ptr(codes), _ptr(scales), M, K, _ptr(t.data), _stream()), "mq_mx_pack")
+    return _with_top(t)
+
+
+def mx_unpack(t: MxTensor):
+    """(codes uint8 [M, K/2], scales uint8 [M, K/32])."""
+    codes = torch.empty((t.rows, t.K // 2), dtype=torch.uint8, device=t.data.device)
+    scales = torch.empty((t.rows, t.K // 32), dtype=torch.uint8, device=t.data.device)
+    _check(load().mq_mx_unpack(_ptr(t.data), t.rows, t.K, _ptr(codes), _ptr(scales), _stream()), "mq_mx_unpack")
+    return codes, scales
+
+
+def mx_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load().mq_mx_linear_workspace_bytes(M, N, K))
+
+
+def mx_linear(x: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+              residual: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, dtype=None) -> torch.Tensor:
+    """Y = mx(X) . W^T + bias (+ residual).  X: [M, K] fp16/bf16, quantised in the call, or an MxTensor; then dtype (fp16 unless out or
+    dtype says otherwise) is the output's.  residual may be out itself.  ws: optional uint8 workspace of mx_linear_workspace_bytes(M, N, K)."""
+    lib = load()
+    packed = isinstance(x, MxTensor)
+    if packed:
+        M, K, device = x.rows, x.K, x.data.device
+        dtype = dtype or (out.dtype if out is not None else torch.float16)
+    else:
+        (M, K), device = _matrix(x).shape, x.device
+        if dtype is not None and dtype != x.dtype:
+            raise TypeError(f"the output has the type of the activations, {x.dtype}")
+        dtype = x.dtype
+    if K != w.K:
+        raise ValueError(f"activations have {K} columns, weights {w.K}")
+    y = _out(out, M, w.rows, dtype, device)
+    dt = _dtype_code(y)
+    if residual is not None:
+        _matrix(residual, M, w.rows, dtype)
+    args = (_ptr(w.data), w.rows, _ptr(_vector(bias, w.rows, dtype, device)), _ptr(y), _ld(y), dt, _ptr(residual), _ld(residual))
+    if packed:
+        _check(lib.mq_mx_linear_codes(_ptr(x.data), M, K, *args, _stream()), "mq_mx_linear_codes")
+    else:
+        ws = _workspace(mx_linear_workspace_bytes(M, w.rows, K), device, ws)
+        _check(lib.mq_mx_linear(_ptr(x), M, K, _ld(x), *args, _ptr(ws), _bytes_of(ws), _stream()), "mq_mx_linear")
+    return y
+
+
+def mx_linear_grad(dy: torch.Tensor, w: MxTensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dX = dY . W, the gradient of mx_linear with respect to its input (the quantisation of X passed straight through)."""
+    M = _matrix(dy, cols=w.rows).shape[0]
+    if w.top is None:
+        raise ValueError("weights without `top`: make them with mx_quantize_weights or mx_pack")
+    dx = _out(out, M, w.K, dy.dtype, dy.device)
+    _check(load().mq_mx_linear_grad(_ptr(dy), M, w.rows, _ld(dy), _ptr(w.data), _ptr(w.top), w.K, _ptr(dx), _ld(dx), _dtype_code(dy), _stream()),
+           "mq_mx_linear_grad")
+    return dx
+
+
+def _params(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor]):
+    p = weight if weight is not None else bias
+    if p is None:
+        return None, None, F32
+    for t in (weight, bias):
+        _vector(t, x.shape[1], p.dtype, x.device)
+    return weight, bias, F32 if p.dtype == torch.float32 else _dtype_code(p)
+
+
+def _stats(x: torch.Tensor, want: bool):
+    if not want:
+        return None, None
+    return torch.empty(x.shape[0], dtype=torch.float32, device=x.device), torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               out: Optional[torch.Tensor] = None, want_stats: bool = False):
+    """Layer norm over the columns of x [M, C] fp16/bf16; weight, bias [C] in 16 bits or float32.  want_stats: (y, mean, rstd), the latter
+    two float32 [M], for layer_norm_grad.  out may be x."""
+    M, N = _matrix(x).shape
+    w, b, pt = _params(x, weight, bias)
+    mean, rstd = _stats(x, want_stats)
+    y = _out(out, M, N, x.dtype, x.device)
+    _check(load().mq_layer_norm(_ptr(x), M, N, _ld(x), _ptr(w), _ptr(b), pt, C.c_float(eps), _ptr(y), _ld(y), _dtype_code(x), _ptr(mean), _ptr(rstd),
+                                _stream()), "mq_layer_norm")
+    return (y, mean, rstd) if want_stats else y
+
+
+def layer_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                  want_stats: bool = False):
+    """Layer norm whose output is quantised to MXFP4 from its float32 values: the input of the mx_linear behind it.  C % 32 == 0."""
+    M, N = _matrix(x).shape
+    w, b, pt = _params(x, weight, bias)
+    mean, rstd = _stats(x, want_stats)
+    t = _new_mx(M, N, x.device)
+    _check(load().mq_layer_norm_mx(_ptr(x), M, N, _ld(x), _ptr(w), _ptr(b), pt, C.c_float(eps), _ptr(t.data), _dtype_code(x), _ptr(mean), _ptr(rstd),
+                                   _stream()), "mq_layer_norm_mx")
+    return (t, mean, rstd) if want_stats else t
+
+
+def layer_norm_grad_workspace_bytes(M: int, N: int) -> int:
+    return int(load().mq_layer_norm_grad_workspace_bytes(M, N))
+
+
+def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                    residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """(dx, dweight, dbias) of layer_norm and layer_norm_mx; dweight and dbias float32 [C].  residual [M, C]: a gradient that reaches x past the norm,
+    added to dx.  out may be dy or residual."""
+    M, N = _matrix(x).shape
+    _matrix(dy, M, N, x.dtype)
+    if residual is not None:
+        _matrix(residual, M, N, x.dtype)
+    w, _, pt = _params(x, weight, None)
+    _vector(mean, M, torch.float32, x.device)
+    _vector(rstd, M, torch.float32, x.device)
+    dx = _out(out, M, N, x.dtype, x.device)
+    sums = torch.empty((2, N), dtype=torch.float32, device=x.device)
+    ws = _workspace(layer_norm_grad_workspace_bytes(M, N), x.device, ws)
+    _check(load().mq_layer_norm_grad(_ptr(dy), _ld(dy), _ptr(x), _ld(x), M, N, _ptr(w), pt, _ptr(mean), _ptr(rstd), _ptr(residual), _ld(residual),
+                                     _ptr(dx), _ld(dx), _dtype_code(x), _ptr(sums[0]), _ptr(sums[1]), _ptr(ws), _bytes_of(ws), _stream()),
+           "mq_layer_norm_grad")
+    return dx, sums[0], sums[1]

@@ -1,0 +1,175 @@
+// C ABI of the microscaled 4-bit linears and of the layer norm: argument validation on the host, workspace carving, launch sequencing.
+#include <math.h>
+
+#include "mx_common.h"
+
+namespace mq {
+
+static inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+static inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+static inline bool type_ok(int dtype) { return dtype == MQ_F16 || dtype == MQ_BF16; }
+
+// A matrix of 16-bit values with `cols` columns: rows may lie apart, and need not start on any boundary but their own type's.
+// (Without rows there is nothing to point to.)
+static int check_matrix(const void* p, int rows, long ld, int cols) {
+    if (ld < cols) return MQ_ERR_BAD_SHAPE;
+    if (rows > 0 && (!p || !aligned(p, 2))) return MQ_ERR_BAD_ARG;
+    return MQ_OK;
+}
+static int check_mx(const void* p, int rows, int K) {
+    if (rows < 0 || K <= 0 || K % 32 != 0 || K > (1 << 21) || rows > (1 << 28)) return MQ_ERR_BAD_SHAPE;
+    if (rows > 0 && (!p || !aligned(p, 256))) return MQ_ERR_BAD_ARG;
+    return MQ_OK;
+}
+
+static int check_product(int M, int N, int K, const void* w, const void* bias, const void* y, long ldy, int dtype, const void* residual, long ldr) {
+    if (!type_ok(dtype)) return MQ_ERR_BAD_ARG;
+    if (M < 0 || N <= 0 || N > (1 << 22)) return MQ_ERR_BAD_SHAPE;
+    int rc;
+    if ((rc = check_mx(w, N, K))) return rc;
+    if (!aligned(bias, 2)) return MQ_ERR_BAD_ARG;
+    if ((rc = check_matrix(y, M, ldy, N))) return rc;
+    if (residual && (rc = check_matrix(residual, M, ldr, N))) return rc;
+    return MQ_OK;
+}
+
+static int product(const void* a, int M, int K, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual, long ldr,
+                   hipStream_t st) {
+    MxGemm g;
+    g.a = mx_view(a, M, K);
+    g.w = mx_view(w, N, K);
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.bias = (const uint16_t*)bias;
+    g.y = (uint16_t*)y;
+    g.ldy = ldy;
+    g.res = (const uint16_t*)residual;
+    g.ldr = ldr;
+    g.dtype = dtype;
+    g.wide = N % 8 == 0 && ldy % 8 == 0 && aligned(y, 16) && (!residual || (ldr % 8 == 0 && aligned(residual, 16)));
+    return launch_mx_gemm(g, st);
+}
+
+static int check_norm(const void* x, int M, int C, long ldx, const void* weight, const void* bias, int param_dtype, int dtype) {
+    if (!type_ok(dtype)) return MQ_ERR_BAD_ARG;
+    if ((weight || bias) && !type_ok(param_dtype) && param_dtype != MQ_F32) return MQ_ERR_BAD_ARG;
+    if (!aligned(weight, param_dtype == MQ_F32 ? 4 : 2) || !aligned(bias, param_dtype == MQ_F32 ? 4 : 2)) return MQ_ERR_BAD_ARG;
+    if (M < 0 || C <= 0 || C > 16384) return MQ_ERR_BAD_SHAPE;
+    return check_matrix(x, M, ldx, C);
+}
+
+}  // namespace mq
+
+using namespace mq;
+
+extern "C" {
+
+size_t mq_mx_bytes(int rows, int K) { return rows < 0 || K <= 0 || K % 32 != 0 ? 0 : mx_bytes(rows, K); }
+
+int mq_mx_quantize(const void* x, int M, int K, long ldx, int dtype, void* mx, void* stream) {
+    if (!type_ok(dtype)) return MQ_ERR_BAD_ARG;
+    int rc;
+    if ((rc = check_mx(mx, M, K)) || (rc = check_matrix(x, M, ldx, K))) return rc;
+    return M == 0 ? MQ_OK : launch_mx_quantize(x, M, K, ldx, dtype, mx, (hipStream_t)stream);
+}
+
+int mq_mx_dequantize(const void* mx, int M, int K, int dtype, void* y, long ldy, void* stream) {
+    if (!type_ok(dtype)) return MQ_ERR_BAD_ARG;
+    int rc;
+    if ((rc = check_mx(mx, M, K)) || (rc = check_matrix(y, M, ldy, K))) return rc;
+    return M == 0 ? MQ_OK : launch_mx_dequantize(mx, M, K, dtype, y, ldy, (hipStream_t)stream);
+}
+
+int mq_mx_pack(const uint8_t* codes, const uint8_t* scales, int M, int K, void* mx, void* stream) {
+    int rc;
+    if ((rc = check_mx(mx, M, K))) return rc;
+    if (M > 0 && (!codes || !scales)) return MQ_ERR_BAD_ARG;
+    return M == 0 ? MQ_OK : launch_mx_pack(codes, scales, M, K, mx, (hipStream_t)stream);
+}
+
+int mq_mx_unpack(const void* mx, int M, int K, uint8_t* codes, uint8_t* scales, void* stream) {
+    int rc;
+    if ((rc = check_mx(mx, M, K))) return rc;
+    if (M > 0 && (!codes || !scales)) return MQ_ERR_BAD_ARG;
+    return M == 0 ? MQ_OK : launch_mx_unpack(mx, M, K, codes, scales, (hipStream_t)stream);
+}
+
+int mq_mx_column_top(const void* mx, int rows, int K, uint8_t* top, void* stream) {
+    int rc;
+    if ((rc = check_mx(mx, rows, K))) return rc;
+    if (!top) return MQ_ERR_BAD_ARG;
+    return launch_mx_column_top(mx, rows, K, top, (hipStream_t)stream);
+}
+
+size_t mq_mx_linear_workspace_bytes(int M, int N, int K) { return M <= 0 || N <= 0 || K <= 0 || K % 32 != 0 ? 0 : up256(mx_bytes(M, K)); }
+
+int mq_mx_linear(const void* x, int M, int K, long ldx, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual,
+                 long ldr, void* ws, size_t ws_bytes, void* stream) {
+    int rc;
+    if ((rc = check_product(M, N, K, w, bias, y, ldy, dtype, residual, ldr)) || (rc = check_matrix(x, M, ldx, K))) return rc;
+    if (M == 0) return MQ_OK;
+    if (!ws || !aligned(ws, 256)) return MQ_ERR_BAD_ARG;
+    if (ws_bytes < mq_mx_linear_workspace_bytes(M, N, K)) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    if ((rc = launch_mx_quantize(x, M, K, ldx, dtype, ws, (hipStream_t)stream))) return rc;
+    return product(ws, M, K, w, N, bias, y, ldy, dtype, residual, ldr, (hipStream_t)stream);
+}
+
+int mq_mx_linear_codes(const void* a, int M, int K, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual, long ldr,
+                       void* stream) {
+    int rc;
+    if ((rc = check_product(M, N, K, w, bias, y, ldy, dtype, residual, ldr)) || (rc = check_mx(a, M, K))) return rc;
+    return M == 0 ? MQ_OK : product(a, M, K, w, N, bias, y, ldy, dtype, residual, ldr, (hipStream_t)stream);
+}
+
+int mq_mx_linear_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* stream) {
+    if (!type_ok(dtype) || !top) return MQ_ERR_BAD_ARG;
+    if (M < 0 || N <= 0 || N > (1 << 22)) return MQ_ERR_BAD_SHAPE;
+    int rc;
+    if ((rc = check_mx(w, N, K)) || (rc = check_matrix(dy, M, lddy, N)) || (rc = check_matrix(dx, M, lddx, K))) return rc;
+    return M == 0 ? MQ_OK : launch_mx_grad(dy, M, N, lddy, w, top, K, dx, lddx, dtype, (hipStream_t)stream);
+}
+
+int mq_layer_norm(const void* x, int M, int C, long ldx, const void* weight, const void* bias, int param_dtype, float eps, void* y, long ldy, int dtype,
+                  float* mean, float* rstd, void* stream) {
+    int rc;
+    if ((rc = check_norm(x, M, C, ldx, weight, bias, param_dtype, dtype)) || (rc = check_matrix(y, M, ldy, C))) return rc;
+    if (!(eps >= 0.0f)) return MQ_ERR_BAD_ARG;
+    if (M == 0) return MQ_OK;
+    NormArgs a = {};
+    a.x = (const uint16_t*)x, a.ldx = ldx, a.M = M, a.C = C, a.weight = weight, a.bias = bias, a.param_dtype = param_dtype, a.eps = eps;
+    a.dtype = dtype, a.mean = mean, a.rstd = rstd, a.y = (uint16_t*)y, a.ldy = ldy;
+    return launch_layer_norm(a, (hipStream_t)stream);
+}
+
+int mq_layer_norm_mx(const void* x, int M, int C, long ldx, const void* weight, const void* bias, int param_dtype, float eps, void* mx, int dtype,
+                     float* mean, float* rstd, void* stream) {
+    int rc;
+    if ((rc = check_norm(x, M, C, ldx, weight, bias, param_dtype, dtype)) || (rc = check_mx(mx, M, C))) return rc;
+    if (!(eps >= 0.0f)) return MQ_ERR_BAD_ARG;
+    if (M == 0) return MQ_OK;
+    NormArgs a = {};
+    a.x = (const uint16_t*)x, a.ldx = ldx, a.M = M, a.C = C, a.weight = weight, a.bias = bias, a.param_dtype = param_dtype, a.eps = eps;
+    a.dtype = dtype, a.mean = mean, a.rstd = rstd, a.mx = mx;
+    return launch_layer_norm_mx(a, (hipStream_t)stream);
+}
+
+size_t mq_layer_norm_grad_workspace_bytes(int M, int C) { return M < 0 || C <= 0 ? 0 : up256(layer_norm_grad_workspace_bytes(M, C)); }
+
+int mq_layer_norm_grad(const void* dy, long lddy, const void* x, long ldx, int M, int C, const void* weight, int param_dtype, const float* mean,
+                       const float* rstd, const void* residual, long ldr, void* dx, long lddx, int dtype, float* dweight, float* dbias, void* ws,
+                       size_t ws_bytes, void* stream) {
+    int rc;
+    if ((rc = check_norm(x, M, C, ldx, weight, nullptr, param_dtype, dtype)) || (rc = check_matrix(dy, M, lddy, C)) || (rc = check_matrix(dx, M, lddx, C)))
+        return rc;
+    if (residual && (rc = check_matrix(residual, M, ldr, C))) return rc;
+    if (M > 0 && (!mean || !rstd || !ws || !aligned(ws, 256))) return MQ_ERR_BAD_ARG;
+    if (ws_bytes < mq_layer_norm_grad_workspace_bytes(M, C)) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    NormArgs a = {};
+    a.x = (const uint16_t*)x, a.ldx = ldx, a.M = M, a.C = C, a.weight = weight, a.param_dtype = param_dtype, a.dtype = dtype;
+    a.mean = (float*)mean, a.rstd = (float*)rstd, a.dy = (const uint16_t*)dy, a.lddy = lddy, a.res = (const uint16_t*)residual, a.ldr = ldr;
+    a.dx = (uint16_t*)dx, a.lddx = lddx, a.dweight = dweight, a.dbias = dbias, a.partial = (float*)ws;
+    return launch_layer_norm_grad(a, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,494 @@
+"""Microscaled 4-bit linears, layer norm and their gradients on the GPU, against the float64 oracle.
+
+Codes, scales and dequantised values are exact.  Other bounds count roundings: a 16-bit result is off by half a step of its type at most, an fp32
+operation by U = 2^-24 of its result, and an addition inside a matrix instruction, which may cut off, by 2 U."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx as omx
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+TYPES = (F16, BF16)
+
+
+@pytest.fixture(scope="module")
+def mq():
+    import paper_2405_17873_amd as m
+    m.load()
+    assert torch.cuda.is_available()
+    return m
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def half_step(y, dtype):
+    """Largest rounding error of a 16-bit value (subnormals of fp16: half of 2^-24)."""
+    return torch.finfo(dtype).eps / 2 * np.abs(y) + (2.0 ** -25 if dtype == F16 else 2.0 ** -133)
+
+
+def rand(shape, dtype, seed, std=1.0, mean=0.0, outliers=True):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g) * std + mean
+    if outliers:
+        x[torch.rand(shape, generator=g) < 0.02] *= 12.0
+    return x.to(dtype).cuda()
+
+
+def spread(t, pad, offset=0):
+    """The same matrix with rows `pad` further apart, `offset` elements into an allocation."""
+    M, K = t.shape
+    flat = torch.full((M * (K + pad) + offset + 8,), float("nan"), dtype=t.dtype, device=t.device)
+    v = flat[offset:offset + M * (K + pad)].view(M, K + pad)[:, :K]
+    v.copy_(t)
+    return v
+
+
+def within(got, want, bound, what="", dtype=None):
+    """dtype: of a rounded result; what lies past its largest value is infinite."""
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    if dtype is not None:
+        big = torch.finfo(dtype).max * (1 + torch.finfo(dtype).eps / 4)  # halfway to the next step
+        past = np.abs(want) >= big
+        assert np.array_equal(got[past], np.copysign(np.inf, want[past])), what
+        got, want = np.where(past, 0.0, got), np.where(past, 0.0, want)
+    assert got.shape == want.shape
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    ok = np.isnan(want) | (np.abs(got - want) <= bound)
+    assert ok.all(), f"{what}: {np.count_nonzero(~ok)} of {ok.size}, first at {np.argwhere(~ok)[0]}, worst {np.nanmax(np.abs(got - want) / np.maximum(bound, 1e-300)):.2f} bounds"
+
+
+# ---------------------------------------------------------------------------------------------------------- conversion
+
+def check_quantize(mq, x):
+    t = mq.mx_quantize(x)
+    codes, scales = (v.cpu().numpy() for v in mq.mx_unpack(t))
+    c, s = omx.quantize(f64(x))
+    assert np.array_equal(scales, s)
+    assert np.array_equal(codes, omx.flat(c))
+    for dtype in TYPES:
+        v = mq.mx_dequantize(t, dtype)
+        with np.errstate(over="ignore"):
+            want = torch.from_numpy(omx.decode(c, s)).to(dtype)
+        assert torch.equal(torch.nan_to_num(v.cpu(), nan=12345.0), torch.nan_to_num(want, nan=12345.0))
+    return t
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K", ((1, 32), (1, 320), (2, 64), (31, 96), (32, 256), (33, 288), (77, 2048), (130, 352), (257, 1952)))
+def test_quantize_exact(mq, M, K, dtype):
+    check_quantize(mq, rand((M, K), dtype, M * 1000 + K))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_quantize_every_pattern(mq, dtype):
+    """All 65536 bit patterns, each under several largest values of its block: borders, ties, subnormals, zeros of both signs, infinities and NaN."""
+    p = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(dtype).float()
+    p = p[torch.isfinite(p)]
+    blocks = []
+    for top in (1.0, 1.5, 6.0, 7.5, 2.0 ** -14, 2.0 ** -20, 0.0):
+        q = p[p.abs() <= (top if top else 1e38)]
+        q = torch.cat([q, torch.zeros(-len(q) % 31)]).view(-1, 31)
+        blocks.append(torch.cat([torch.full((len(q), 1), top), q], 1))
+    x = torch.cat(blocks).to(dtype)
+    x[5, 3], x[6, 0], x[7, 31] = float("inf"), float("-inf"), float("nan")
+    x[8] = 0.0
+    x[9] = -0.0
+    check_quantize(mq, x.cuda())
+    check_quantize(mq, x[:len(x) // 64 * 64].reshape(-1, 2048).cuda())
+
+
+@pytest.mark.parametrize("pad,offset", ((0, 1), (1, 0), (8, 8), (3, 5), (40, 4)))
+def test_quantize_views(mq, pad, offset):
+    x = rand((37, 160), F16, 3)
+    v = spread(x, pad, offset)
+    t = check_quantize(mq, v)
+    out = spread(torch.zeros(37, 160, dtype=F16, device="cuda"), pad, offset)
+    mq.mx_dequantize(t, F16, out=out)
+    assert torch.equal(out, mq.mx_dequantize(t, F16))
+
+
+def test_pack_round_trip_and_top(mq):
+    rng = np.random.default_rng(4)
+    codes = torch.from_numpy(rng.integers(0, 256, (45, 80), dtype=np.uint8)).cuda()
+    scales = torch.from_numpy(rng.integers(90, 140, (45, 5), dtype=np.uint8)).cuda()
+    scales[3, 2], scales[:, 4] = 255, 255
+    t = mq.mx_pack(codes, scales)
+    c, s = mq.mx_unpack(t)
+    assert torch.equal(s, scales)
+    nan = (scales == 255).repeat_interleave(16, 1)
+    assert torch.equal(c, torch.where(nan, 0, codes))
+    finite = np.where(scales.cpu().numpy() == 255, 0, scales.cpu().numpy())
+    assert np.array_equal(t.top.cpu().numpy(), finite.max(0))
+
+
+def test_quantize_many_rows(mq):
+    """More groups of 32 rows than one grid dimension holds."""
+    M = 65535 * 32 + 37
+    x = torch.zeros(M, 32, dtype=F16, device="cuda")
+    tail = rand((64, 32), F16, 5)
+    x[-64:] = tail
+    t = mq.mx_quantize(x)
+    v = mq.mx_dequantize(t, F16)
+    assert torch.equal(v[-64:].cpu(), torch.from_numpy(omx.values(f64(tail))).half())
+    assert not v[:-64].any()
+
+
+# ------------------------------------------------------------------------------------------------------------- linear
+
+def check_linear(mq, x, w, bias=None, res=None, out=None, packed=False):
+    wq = mq.mx_quantize_weights(w)
+    if packed:
+        y = mq.mx_linear(mq.mx_quantize(x), wq, bias, residual=res, dtype=x.dtype, out=out)
+    else:
+        y = mq.mx_linear(x, wq, bias, residual=res, out=out)
+    r64 = None if res is None else f64(res)
+    want, mag = omx.linear(omx.values(f64(x)), omx.values(f64(w)), None if bias is None else f64(bias), r64)
+    K = x.shape[1]
+    acc = (K + 4) * 2 * U * mag
+    within(f64(y), want, acc + half_step(np.abs(want) + acc, x.dtype), f"{tuple(x.shape)} x {w.shape[0]}", x.dtype)
+    return y
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K,N", ((1, 32, 1), (1, 320, 1280), (1, 64, 33), (2, 96, 8), (3, 5120, 40), (8, 2048, 640), (16, 352, 64), (17, 256, 130),
+                                   (32, 1280, 96), (33, 288, 31), (64, 640, 320), (77, 2048, 100), (100, 480, 257), (129, 128, 129), (260, 1952, 520),
+                                   (513, 320, 384), (700, 64, 1000)))
+def test_linear(mq, M, K, N, dtype):
+    x, w, b = rand((M, K), dtype, M + K + N), rand((N, K), dtype, N, 0.02), rand((N,), dtype, 9, 0.1)
+    check_linear(mq, x, w, b)
+    check_linear(mq, x, w, None, rand((M, N), dtype, 10), packed=True)
+
+
+@pytest.mark.parametrize("M", (1, 5, 40, 200))
+def test_linear_views(mq, M):
+    """Strides and alignments of every operand; the residual as the output itself; the output over the activations."""
+    K, N = 160, 72
+    x, w, b, r = rand((M, K), F16, 1), rand((N, K), F16, 2, 0.05), rand((N,), F16, 3), rand((M, N), F16, 4)
+    want = check_linear(mq, x, w, b, r)
+    wq = mq.mx_quantize_weights(w)
+    for pad, offset in ((8, 8), (1, 0), (5, 3), (16, 4)):
+        o = spread(torch.zeros_like(r), pad, offset)
+        base = o._base if o._base is not None else o
+        mq.mx_linear(spread(x, pad, offset), wq, spread(b.view(1, -1), pad, offset)[0], out=o, residual=spread(r, pad, offset))
+        assert torch.equal(o, want)
+        assert int(torch.isnan(base).sum()) == base.numel() - M * N  # nothing beside the result
+    o = r.clone()
+    assert mq.mx_linear(x, wq, b, out=o, residual=o) is o and torch.equal(o, want)
+    both = torch.zeros(M, K, dtype=F16, device="cuda")
+    both.copy_(x)
+    mq.mx_linear(both, wq, b, residual=r, out=both[:, 8:8 + N])
+    assert torch.equal(both[:, 8:8 + N], want)
+
+
+@pytest.mark.parametrize("M", (1, 20, 150))
+def test_linear_special_values(mq, M):
+    K, N = 320, 64
+    x, w = rand((M, K), F16, 6), rand((N, K), F16, 7, 0.02)
+    x[0] = 0.0
+    if M > 4:
+        x[1, 5], x[2, 319], x[3] = float("nan"), float("inf"), 60000.0
+        x[4, 64:96] = 2.0 ** -24
+    w[3], w[5, 40] = 0.0, float("nan")
+    y = f64(check_linear(mq, x, w))
+    assert np.isnan(y[:, 5]).all() and (y[0, 3] == 0.0)
+    if M > 4:
+        assert np.isnan(y[1]).all() and np.isnan(y[2]).all() and np.isfinite(y[4, :5]).all()
+
+
+def test_linear_deterministic_and_independent_of_neighbours(mq):
+    """The same bits twice; a row's result does not depend on the rows beside it."""
+    x, w = rand((70, 640), BF16, 8), rand((200, 640), BF16, 9, 0.02)
+    wq = mq.mx_quantize_weights(w)
+    y = mq.mx_linear(x, wq)
+    assert torch.equal(y, mq.mx_linear(x, wq))
+    x2 = x.clone()
+    x2[1:] = float("nan")
+    assert torch.equal(mq.mx_linear(x2, wq)[0], y[0])
+
+
+def test_empty(mq):
+    w = mq.mx_quantize_weights(rand((8, 64), F16, 1))
+    x = torch.empty(0, 64, dtype=F16, device="cuda")
+    assert mq.mx_linear(x, w).shape == (0, 8)
+    assert mq.mx_linear(mq.mx_quantize(x), w).shape == (0, 8)
+    assert mq.mx_linear_grad(torch.empty(0, 8, dtype=F16, device="cuda"), w).shape == (0, 64)
+    y, mean, rstd = mq.layer_norm(x, want_stats=True)
+    assert y.shape == (0, 64) and mean.shape == (0,)
+    dx, dw, db = mq.layer_norm_grad(x, x, None, mean, rstd)
+    assert dx.shape == (0, 64) and not dw.any() and not db.any() and dw.shape == (64,)
+    assert mq.mx_dequantize(mq.layer_norm_mx(x)).shape == (0, 64)
+
+
+def test_linear_offsets_past_32_bits(mq):
+    """An output of more than 2^31 elements, and activations of more than 2^32 bytes: rows from both ends and the middle."""
+    M, K, N = 70001, 32768, 32768
+    x = torch.empty(M, K, dtype=F16, device="cuda")
+    rows = [0, 1, 32767, 32768, 65535, 65536, 70000]
+    x.fill_(1.0)
+    some = rand((len(rows), K), F16, 11)
+    x[rows] = some
+    w = rand((N, K), F16, 12, 0.02)
+    wq = mq.mx_quantize_weights(w)
+    y = mq.mx_linear(x, wq)
+    cols = torch.arange(0, N, 257)
+    want, mag = omx.linear(omx.values(f64(some)), omx.values(f64(w[cols.cuda()])))
+    acc = (K + 4) * 2 * U * mag
+    within(f64(y[rows][:, cols.cuda()]), want, acc + half_step(np.abs(want) + acc, F16))
+    dx = mq.mx_linear_grad(y, wq)
+    g = f64(y[rows])
+    kk = torch.arange(0, K, 509)
+    want, mag = omx.linear_grad(g, omx.values(f64(w))[:, kk.numpy()])
+    acc = (N + 8) * 2 * U * mag
+    within(f64(dx[rows][:, kk.cuda()]), want, acc + half_step(np.abs(want) + acc, F16))
+
+
+# --------------------------------------------------------------------------------------------------- gradient of linear
+
+def check_grad(mq, dy, w, out=None):
+    wq = mq.mx_quantize_weights(w)
+    dx = mq.mx_linear_grad(dy, wq, out=out)
+    v = omx.values(f64(w))
+    want, mag = omx.linear_grad(f64(dy), v)
+    top = np.nanmax(np.abs(v).reshape(v.shape[0], -1, 32), axis=(0, 2), initial=0.0)
+    # products exact in fp32, N additions; what lies 2^-37 below a block column's largest may be missing (64 times that: 6 units against the scale)
+    acc = (w.shape[0] + 8) * 2 * U * mag + np.abs(f64(dy)).sum(1, keepdims=True) * np.repeat(top, 32)[None] * 2.0 ** -36
+    within(f64(dx), want, acc + half_step(np.abs(want) + acc, dy.dtype), f"{tuple(dy.shape)} x {w.shape[1]}", dy.dtype)
+    return dx
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K,N", ((1, 32, 1), (1, 1280, 320), (2, 64, 7), (31, 96, 33), (33, 352, 64), (64, 64, 65), (77, 2048, 100), (130, 320, 640),
+                                   (257, 480, 130), (300, 160, 1001)))
+def test_linear_grad(mq, M, K, N, dtype):
+    check_grad(mq, rand((M, N), dtype, M + N), rand((N, K), dtype, K, 0.02))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_grad_scales(mq, dtype):
+    """Weights from the smallest scale to the largest, in one column of blocks and across them."""
+    w = rand((96, 256), dtype, 20)
+    e = torch.linspace(-20, 8, 96).round() if dtype == F16 else torch.linspace(-120, 100, 96).round()
+    w[:, :128] *= 2.0 ** e.view(-1, 1).to(dtype).cuda()
+    w[:, 128:160] *= 2.0 ** -14 if dtype == F16 else 2.0 ** -125
+    w[:, 160:192] = 0.0
+    w[:, 192:224] *= 1000.0 if dtype == F16 else 1e30
+    dy = rand((40, 96), dtype, 21)
+    if dtype == BF16:
+        dy *= 2.0 ** -10
+    check_grad(mq, dy, w)
+
+
+def test_linear_grad_views_and_special_values(mq):
+    M, K, N = 45, 160, 72
+    dy, w = rand((M, N), F16, 22), rand((N, K), F16, 23, 0.05)
+    want = check_grad(mq, dy, w)
+    wq = mq.mx_quantize_weights(w)
+    for pad, offset in ((8, 8), (1, 0), (5, 3)):
+        o = spread(torch.zeros(M, K, dtype=F16, device="cuda"), pad, offset)
+        mq.mx_linear_grad(spread(dy, pad, offset), wq, out=o)  # (what lies between the rows is NaN)
+        assert torch.equal(o, want)
+        assert int(torch.isnan(o._base).sum()) == o._base.numel() - M * K
+    dy[3], dy[7, 5], w[9, 40] = 0.0, float("nan"), float("inf")
+    dx = f64(check_grad(mq, dy, w))
+    assert np.isnan(dx[7]).all() and np.isnan(dx[:, 32:64]).all() and (dx[3, :32] == 0).all()
+
+
+def test_linear_grad_wants_top(mq):
+    with pytest.raises(ValueError):
+        mq.mx_linear_grad(rand((2, 8), F16, 1), mq.mx_quantize(rand((8, 64), F16, 1)))
+
+
+# ---------------------------------------------------------------------------------------------------------- layer norm
+
+def depth(C):
+    """Additions on the way of one value into a row's sum: up to 64 in a lane, 6 over lanes, 3 over waves."""
+    return 64 + 9
+
+
+def norm_bounds(x, w, eps):
+    """(mean, rstd, bound of mean, relative bound of rstd) of the fp32 statistics."""
+    mean, rstd = omx.norm_stats(x, eps)
+    dm = (depth(x.shape[1]) + 2) * U * np.abs(x).mean(-1, keepdims=True)
+    var = 1.0 / rstd ** 2
+    dv = ((depth(x.shape[1]) + 5) * U * (var - eps) + dm ** 2) / var
+    return mean, rstd, dm, 0.5 * dv + 4 * U
+
+
+def norm_error(x, w, b, eps):
+    """(exact normalised values, bound of their fp32 form)."""
+    mean, rstd, dm, dr = norm_bounds(x, w, eps)
+    d = x - mean
+    y = d * rstd * w + b
+    err = np.abs(w) * rstd * (dm + np.abs(d) * (dr + 4 * U)) + U * (np.abs(y) + np.abs(b) + np.abs(d * rstd * w))
+    return y, err
+
+
+def params(C, kind, dtype, seed):
+    if kind == "none":
+        return None, None
+    t = F32 if kind == "f32" else dtype
+    return rand((C,), F32, seed, 0.2, 1.0, False).to(t), rand((C,), F32, seed + 1, 0.2, 0.0, False).to(t)
+
+
+def p64(w, b, C):
+    return (np.ones(C) if w is None else f64(w)), (np.zeros(C) if b is None else f64(b))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,C", ((1, 1), (1, 320), (3, 8), (5, 33), (2, 255), (33, 512), (7, 520), (4, 1000), (9, 1280), (5, 1529), (6, 2048), (3, 2056),
+                                 (2, 4099), (3, 8192), (2, 16384), (70, 640)))
+@pytest.mark.parametrize("kind", ("16", "f32", "none"))
+def test_layer_norm(mq, M, C, dtype, kind):
+    x = rand((M, C), dtype, M + C, 1.0, 0.5)
+    w, b = params(C, kind, dtype, 30)
+    y, mean, rstd = mq.layer_norm(x, w, b, 1e-5, want_stats=True)
+    X = f64(x)
+    want, err = norm_error(X, *p64(w, b, C), 1e-5)
+    within(f64(y), want, err + half_step(np.abs(want) + err, dtype))
+    m, r, dm, dr = norm_bounds(X, None, 1e-5)
+    within(f64(mean)[:, None], m, dm)
+    within(f64(rstd)[:, None], r, r * dr)
+
+
+def test_layer_norm_views_and_special_rows(mq):
+    M, C = 9, 168
+    x = rand((M, C), F16, 31)
+    x[1] = 3.0          # no variance
+    x[2] = 0.0
+    x[3, 7], x[4, 0] = float("nan"), float("inf")
+    x[5] = 60000.0
+    x[5, ::2] = -60000.0
+    x[6] = 2.0 ** -24
+    w, b = params(C, "16", F16, 32)
+    y = mq.layer_norm(x, w, b, 1e-5)
+    Y = f64(y)
+    assert np.isnan(Y[3]).all() and np.isnan(Y[4]).all()
+    ok = [0, 1, 2, 5, 6, 7, 8]
+    want, err = norm_error(f64(x)[ok], *p64(w, b, C), 1e-5)
+    within(Y[ok], want, err + half_step(np.abs(want) + err, F16))
+    for pad, offset in ((8, 8), (1, 0), (5, 3)):
+        o = spread(torch.zeros_like(x), pad, offset)
+        mq.layer_norm(spread(x, pad, offset), spread(w.view(1, -1), 0, offset)[0], spread(b.view(1, -1), 0, offset)[0], 1e-5, out=o)
+        assert torch.equal(torch.nan_to_num(o), torch.nan_to_num(y))
+    z = x.clone()
+    mq.layer_norm(z, w, b, 1e-5, out=z)
+    assert torch.equal(torch.nan_to_num(z), torch.nan_to_num(y))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,C,kind", ((1, 32, "16"), (1, 320, "f32"), (31, 96, "none"), (33, 640, "16"), (40, 1280, "f32"), (5, 2080, "16"), (3, 4096, "f32"),
+                                      (2, 8224, "none"), (2, 16384, "16"), (65, 512, "16")))
+def test_layer_norm_mx(mq, M, C, kind, dtype):
+    """The kernel quantises fp32 values that lie within `err` of the exact ones: its scale is that of some such block, its codes lie between those
+    of the interval's ends under that scale."""
+    x = rand((M, C), dtype, M + C, 1.0, 0.3)
+    w, b = params(C, kind, dtype, 33)
+    t, mean, rstd = mq.layer_norm_mx(x, w, b, 1e-5, want_stats=True)
+    codes, scales = (v.cpu().numpy() for v in mq.mx_unpack(t))
+    y, err = norm_error(f64(x), *p64(w, b, C), 1e-5)
+    lo, hi = np.maximum(np.abs(y) - err, 0.0), np.abs(y) + err
+    assert (scales >= omx.scale_bytes(lo)).all() and (scales <= omx.scale_bytes(hi)).all()
+    got = omx.decode(omx.unflat(codes), scales)
+    assert (got >= omx.decode(omx.encode(y - err, scales), scales)).all() and (got <= omx.decode(omx.encode(y + err, scales), scales)).all()
+    _, m2, r2 = mq.layer_norm(x, w, b, 1e-5, want_stats=True)
+    assert torch.equal(mean, m2) and torch.equal(rstd, r2)
+    # what is padding adds nothing to a product: the whole buffer beyond the real blocks is zero
+    data = t.data.cpu().numpy()
+    assert np.count_nonzero(data) <= np.count_nonzero(codes) + np.count_nonzero(scales)
+
+
+def test_layer_norm_mx_into_linear(mq):
+    """Rows with NaN stay what they are, and spoil no other row."""
+    x, w = rand((70, 640), F16, 34), rand((96, 640), F16, 35, 0.02)
+    g, s = params(640, "16", F16, 36)
+    wq = mq.mx_quantize_weights(w)
+    clean = mq.mx_linear(mq.layer_norm_mx(x, g, s), wq)
+    x[5, 9], x[69, 3] = float("nan"), float("inf")
+    y = mq.mx_linear(mq.layer_norm_mx(x, g, s), wq)
+    assert torch.isnan(y[[5, 69]]).all()
+    rest = [i for i in range(70) if i not in (5, 69)]
+    assert torch.equal(y[rest], clean[rest])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,C", ((1, 1), (1, 320), (3, 8), (5, 33), (33, 512), (7, 520), (4, 1000), (300, 1280), (6, 2048), (3, 2056), (2, 4099), (3, 8192),
+                                 (2, 16384), (2500, 640), (5000, 40)))
+@pytest.mark.parametrize("kind,residual", (("16", False), ("f32", True), ("none", True)))
+def test_layer_norm_grad(mq, M, C, dtype, kind, residual):
+    x, dy = rand((M, C), dtype, M + C, 1.0, 0.5), rand((M, C), dtype, M + C + 1)
+    res = rand((M, C), dtype, 40) if residual else None
+    w, b = params(C, kind, dtype, 41)
+    _, mean, rstd = mq.layer_norm(x, w, b, 1e-5, want_stats=True)
+    dx, dw, db = mq.layer_norm_grad(dy, x, w, mean, rstd, residual=res)
+    W, _ = p64(w, b, C)
+    X, DY, mu, r = f64(x), f64(dy), f64(mean)[:, None], f64(rstd)[:, None]  # the statistics are inputs, taken as they are
+    wantx, wantw, wantb = omx.norm_grad(DY, X, W, mu, r, None if res is None else f64(res))
+    xh, g = (X - mu) * r, DY * W
+    exh = 3 * U * (np.abs(X) + np.abs(mu)) * r
+    n = depth(C)
+    m1, m2 = np.abs(g).mean(-1, keepdims=True), (np.abs(g) * (np.abs(xh) + exh)).mean(-1, keepdims=True)
+    e1, e2 = (n + 4) * U * m1, (n + 6) * U * m2 + (np.abs(g) * exh).mean(-1, keepdims=True)
+    err = r * (6 * U * (np.abs(g) + m1 + np.abs(xh) * m2) + e1 + np.abs(xh) * e2 + exh * m2) + (2 * U * np.abs(f64(res)) if residual else 0) + 2 * U * np.abs(wantx)
+    within(f64(dx), wantx, err + half_step(np.abs(wantx) + err, dtype), "dx")
+    # rows of a workgroup's walk (M / 2048 of them, or all), 4 waves, then up to 32 workgroups in a run and 16 runs
+    rows = M / 256 + 64
+    within(f64(dw), wantw, ((rows + 2) * U * np.abs(DY * xh) + np.abs(DY) * exh).sum(0) + 2.0 ** -126, "dweight")
+    within(f64(db), wantb, rows * U * np.abs(DY).sum(0) + 2.0 ** -126, "dbias")
+
+
+def test_layer_norm_grad_views_and_aliases(mq):
+    M, C = 50, 168
+    x, dy, res = rand((M, C), F16, 42), rand((M, C), F16, 43), rand((M, C), F16, 44)
+    w, b = params(C, "16", F16, 45)
+    _, mean, rstd = mq.layer_norm(x, w, b, want_stats=True)
+    want = mq.layer_norm_grad(dy, x, w, mean, rstd, residual=res)
+    for pad, offset in ((8, 8), (1, 0), (5, 3)):
+        o = spread(torch.zeros_like(x), pad, offset)
+        got = mq.layer_norm_grad(spread(dy, pad, offset), spread(x, pad, offset), w, mean, rstd, residual=spread(res, pad, offset), out=o)
+        assert all(torch.equal(a, c) for a, c in zip(got, want))
+    for alias in ("dy", "res"):
+        d, r = dy.clone(), res.clone()
+        got = mq.layer_norm_grad(d, x, w, mean, rstd, residual=r, out=d if alias == "dy" else r)
+        assert all(torch.equal(a, c) for a, c in zip(got, want))
+
+
+# ------------------------------------------------------------------------------------------------- streams and graphs
+
+def step(mq, x, gain, shift, wq, bias, dy, res):
+    """Forward and backward of a norm and the linear behind it."""
+    t, mean, rstd = mq.layer_norm_mx(x, gain, shift, want_stats=True)
+    y = mq.mx_linear(t, wq, bias, dtype=x.dtype)
+    dn = mq.mx_linear_grad(dy, wq)
+    return (y,) + tuple(mq.layer_norm_grad(dn, x, gain, mean, rstd, residual=res)) + (mq.mx_linear(x, wq, bias, residual=dy),)
+
+
+def test_graph_replays_and_side_stream(mq):
+    M, C, N = 130, 320, 264
+    make = lambda s: (rand((M, C), F16, s), rand((M, N), F16, s + 1), rand((M, C), F16, s + 2))
+    gain, shift = params(C, "f32", F16, 50)
+    wq, bias = mq.mx_quantize_weights(rand((N, C), F16, 51, 0.02)), rand((N,), F16, 52)
+    x, dy, res = make(60)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        eager = step(mq, x, gain, shift, wq, bias, dy, res)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for a, c in zip(eager, step(mq, x, gain, shift, wq, bias, dy, res)):
+        assert torch.equal(a, c)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(mq, x, gain, shift, wq, bias, dy, res)
+    for s in (60, 70, 80, 60):
+        for t, v in zip((x, dy, res), make(s)):
+            t.copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, c in zip(captured, step(mq, x, gain, shift, wq, bias, dy, res)):
+            assert torch.equal(a, c)
