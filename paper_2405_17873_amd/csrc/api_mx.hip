@@ -47,7 +47,7 @@ static int product(const void* a, int M, int K, const void* w, int N, const void
     g.res = (const uint16_t*)residual;
     g.ldr = ldr;
     g.dtype = dtype;
-    g.wide = N % 8 == 0 && ldy % 8 == 0 && aligned(y, 16) && (!residual || (ldr % 8 == 0 && aligned(residual, 16)));
+    g.wide = N % 8 == 0 && ldy % 8 == 0 && aligned(y, 16) && (!residual || (ldr % 8 == 0 && aligned(residual, 16))) && aligned(bias, 8);
     return launch_mx_gemm(g, st);
 }
 

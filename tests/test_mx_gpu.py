@@ -242,8 +242,8 @@ def test_linear_offsets_past_32_bits(mq):
     within(f64(y[rows][:, cols.cuda()]), want, acc + half_step(np.abs(want) + acc, F16))
     dx = mq.mx_linear_grad(y, wq)
     g = f64(y[rows])
-    kk = torch.arange(0, K, 509)
-    want, mag = omx.linear_grad(g, omx.values(f64(w))[:, kk.numpy()])
+    kk = torch.cat([torch.arange(k, k + 32) for k in (0, 1024, K // 2, K - 32)])  # whole blocks
+    want, mag = omx.linear_grad(g, omx.values(f64(w[:, kk.cuda()])))
     acc = (N + 8) * 2 * U * mag
     within(f64(dx[rows][:, kk.cuda()]), want, acc + half_step(np.abs(want) + acc, F16))
 
