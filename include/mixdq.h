@@ -438,7 +438,9 @@ int mq_mx_linear_codes(const void* a, int M, int K, const void* w, int N, const 
 
 /* Gradient of mq_mx_linear with respect to X, the quantisation of X passed straight through: dX = dY W, dY [M,N], dX [M,K] of dtype, sums fp32,
  * rounded once.  top: mq_mx_column_top of W.  Weights below 2^-37 (bfloat16: 2^-128) of the largest of their block column may be taken as zero. */
-int mq_mx_linear_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* stream);
+size_t mq_mx_linear_grad_workspace_bytes(int M, int N, int K); /* 0: none is needed, ws may be null */
+int mq_mx_linear_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* ws,
+                      size_t ws_bytes, void* stream);
 
 /* Y = (X - mean) rstd weight + bias over the C columns of each row, rstd = 1 / sqrt(variance + eps), variance = mean of squared deviations.  weight,
  * bias [C] of param_dtype (MQ_F16, MQ_BF16 or MQ_F32), each nullable (1 and 0).  mean, rstd [M]: nullable outputs, for the gradient.  Sums fp32.

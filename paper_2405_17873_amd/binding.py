@@ -29,7 +29,7 @@ EXPORTS = ("mq_version", "mq_last_hip_error", "mq_tune_force_tile", "mq_tune_for
            "mq_conv_tap_sums", "mq_conv3x3_a8_workspace_bytes", "mq_conv3x3_a8",
            "mq_bos_aware_kv_proj_workspace_bytes", "mq_bos_aware_kv_proj", "mq_alloc_solve", "mq_alloc_split_budget",
            "mq_alloc_search", "mq_mx_bytes", "mq_mx_quantize", "mq_mx_dequantize", "mq_mx_pack", "mq_mx_unpack", "mq_mx_column_top",
-           "mq_mx_linear_workspace_bytes", "mq_mx_linear", "mq_mx_linear_codes", "mq_mx_linear_grad", "mq_layer_norm", "mq_layer_norm_mx",
+           "mq_mx_linear_workspace_bytes", "mq_mx_linear", "mq_mx_linear_codes", "mq_mx_linear_grad_workspace_bytes", "mq_mx_linear_grad", "mq_layer_norm", "mq_layer_norm_mx",
            "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad")
 
 
@@ -62,7 +62,7 @@ def load():
             raise RuntimeError(f"{_LIB_PATH} is missing: run `python -c 'import __graft_entry__ as g; g.build()'`")
         lib = C.CDLL(_LIB_PATH)
         for name in ("mq_a8_row_bytes", "mq_split_workspace_bytes", "mq_builtin_workspace_bytes", "mq_conv3x3_a8_workspace_bytes", "mq_packed_bytes", "mq_qlinear_a8_workspace_bytes", "mq_qlinear_a8_geglu_dynamic_workspace_bytes", "mq_bos_aware_kv_proj_workspace_bytes",
-                     "mq_mx_bytes", "mq_mx_linear_workspace_bytes", "mq_layer_norm_grad_workspace_bytes"):
+                     "mq_mx_bytes", "mq_mx_linear_workspace_bytes", "mq_mx_linear_grad_workspace_bytes", "mq_layer_norm_grad_workspace_bytes"):
             getattr(lib, name).restype = C.c_size_t
         lib.mq_prof_bracket_overhead_us.restype = C.c_double
         _lib = lib
@@ -875,14 +875,20 @@ def mx_linear(x: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[torc
     return y
 
 
-def mx_linear_grad(dy: torch.Tensor, w: MxTensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """dX = dY . W, the gradient of mx_linear with respect to its input (the quantisation of X passed straight through)."""
-    M = _matrix(dy, cols=w.rows).shape[0]
+def mx_linear_grad_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load().mq_mx_linear_grad_workspace_bytes(M, N, K))
+
+
+def mx_linear_grad(dy: torch.Tensor, w: MxTensor, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dX = dY . W, the gradient of mx_linear with respect to its input (the quantisation of X passed straight through).  ws: optional uint8
+    workspace of mx_linear_grad_workspace_bytes(M, N, K)."""
+    M, N = _matrix(dy, cols=w.rows).shape
     if w.top is None:
         raise ValueError("weights without `top`: make them with mx_quantize_weights or mx_pack")
     dx = _out(out, M, w.K, dy.dtype, dy.device)
-    _check(load().mq_mx_linear_grad(_ptr(dy), M, w.rows, _ld(dy), _ptr(w.data), _ptr(w.top), w.K, _ptr(dx), _ld(dx), _dtype_code(dy), _stream()),
-           "mq_mx_linear_grad")
+    ws = _workspace(mx_linear_grad_workspace_bytes(M, N, w.K), dy.device, ws)
+    _check(load().mq_mx_linear_grad(_ptr(dy), M, N, _ld(dy), _ptr(w.data), _ptr(w.top), w.K, _ptr(dx), _ld(dx), _dtype_code(dy), *_ws_args(ws),
+                                    _stream()), "mq_mx_linear_grad")
     return dx
 
 

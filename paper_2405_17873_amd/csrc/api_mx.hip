@@ -122,12 +122,19 @@ int mq_mx_linear_codes(const void* a, int M, int K, const void* w, int N, const 
     return M == 0 ? MQ_OK : product(a, M, K, w, N, bias, y, ldy, dtype, residual, ldr, (hipStream_t)stream);
 }
 
-int mq_mx_linear_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* stream) {
+size_t mq_mx_linear_grad_workspace_bytes(int M, int N, int K) { return M <= 0 || N <= 0 || K <= 0 || K % 32 != 0 ? 0 : up256(mx_grad_workspace_bytes(M, N, K)); }
+
+int mq_mx_linear_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* ws,
+                      size_t ws_bytes, void* stream) {
     if (!type_ok(dtype) || !top) return MQ_ERR_BAD_ARG;
     if (M < 0 || N <= 0 || N > (1 << 22)) return MQ_ERR_BAD_SHAPE;
     int rc;
     if ((rc = check_mx(w, N, K)) || (rc = check_matrix(dy, M, lddy, N)) || (rc = check_matrix(dx, M, lddx, K))) return rc;
-    return M == 0 ? MQ_OK : launch_mx_grad(dy, M, N, lddy, w, top, K, dx, lddx, dtype, (hipStream_t)stream);
+    if (M == 0) return MQ_OK;
+    const size_t need = mq_mx_linear_grad_workspace_bytes(M, N, K);
+    if (need > 0 && (!ws || !aligned(ws, 256))) return MQ_ERR_BAD_ARG;
+    if (ws_bytes < need) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    return launch_mx_grad(dy, M, N, lddy, w, top, K, dx, lddx, dtype, ws, (hipStream_t)stream);
 }
 
 int mq_layer_norm(const void* x, int M, int C, long ldx, const void* weight, const void* bias, int param_dtype, float eps, void* y, long ldy, int dtype,

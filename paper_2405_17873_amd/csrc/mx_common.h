@@ -149,7 +149,9 @@ int launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int M, int K, vo
 int launch_mx_unpack(const void* mx, int M, int K, uint8_t* codes, uint8_t* scales, hipStream_t st);
 int launch_mx_column_top(const void* mx, int rows, int K, uint8_t* top, hipStream_t st);
 int launch_mx_gemm(const MxGemm& g, hipStream_t st);
-int launch_mx_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, hipStream_t st);
+int launch_mx_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* ws,
+                   hipStream_t st);
+size_t mx_grad_workspace_bytes(long M, long N, long K);
 
 struct NormArgs {
     const uint16_t* x;

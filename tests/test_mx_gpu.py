@@ -264,7 +264,8 @@ def check_grad(mq, dy, w, out=None):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("M,K,N", ((1, 32, 1), (1, 1280, 320), (2, 64, 7), (31, 96, 33), (33, 352, 64), (64, 64, 65), (77, 2048, 100), (130, 320, 640),
-                                   (257, 480, 130), (300, 160, 1001)))
+                                   (257, 480, 130), (300, 160, 1001),
+                                   (1, 160, 9000), (20, 608, 4104), (50, 1280, 5000), (100, 96, 8200), (400, 2080, 1320)))
 def test_linear_grad(mq, M, K, N, dtype):
     check_grad(mq, rand((M, N), dtype, M + N), rand((N, K), dtype, K, 0.02))
 

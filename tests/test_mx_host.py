@@ -121,9 +121,12 @@ def test_error_codes_without_a_gpu(lib):
     assert lin(wsb=100) == -4
     code = lambda a=p, M=4, K=64, y=p, ldy=8: lib.mq_mx_linear_codes(a, M, K, p, 8, null, y, L(ldy), 0, null, L(0), st)
     assert code(a=null) == -1 and code(a=off) == -1 and code(y=null) == -1 and code(ldy=4) == -2 and code(K=63) == -2
-    gr = lambda dy=p, M=4, N=8, ld=8, w=p, top=p, K=64, dx=p, lddx=64, dt=0: lib.mq_mx_linear_grad(dy, M, N, L(ld), w, top, K, dx, L(lddx), dt, st)
+    gr = lambda dy=p, M=4, N=8, ld=8, w=p, top=p, K=64, dx=p, lddx=64, dt=0, ws=null, wsb=0: lib.mq_mx_linear_grad(
+        dy, M, N, L(ld), w, top, K, dx, L(lddx), dt, ws, C.c_size_t(wsb), st)
     assert gr(dy=null) == -1 and gr(w=null) == -1 and gr(top=null) == -1 and gr(dx=null) == -1 and gr(dt=3) == -1
     assert gr(M=-1) == -2 and gr(N=0) == -2 and gr(K=31) == -2 and gr(ld=7) == -2 and gr(lddx=63) == -2
+    need = lib.mq_mx_linear_grad_workspace_bytes(4, 16384, 64)  # a long reduction of few results is cut into parts
+    assert need > 0 and gr(N=16384, ld=16384) == -1 and gr(N=16384, ld=16384, ws=p, wsb=need - 1) == -4 and gr(N=16384, ld=16384, ws=off, wsb=need) == -1
     f = C.c_float
     ln = lambda x=p, M=4, N=64, ld=64, w=null, b=null, pt=2, eps=1e-5, y=p, ldy=64, dt=0: lib.mq_layer_norm(
         x, M, N, L(ld), w, b, pt, f(eps), y, L(ldy), dt, null, null, st)
