@@ -427,7 +427,8 @@ int mq_mx_unpack(const void* mx, int M, int K, uint8_t* codes, uint8_t* scales, 
 int mq_mx_column_top(const void* mx, int rows, int K, uint8_t* top, void* stream);
 
 /* Y = mx(X) W^T + bias (+ residual), X [M,K] and Y [M,N] of dtype, W a microscaled matrix [N,K], bias [N] of dtype (nullable), residual [M,N] of
- * dtype (nullable; may be Y itself).  X is quantised in the call; products and sums are fp32, rounded once.  Y may overlap X. */
+ * dtype (nullable; may be Y itself).  X is quantised in the call; products and sums are fp32, rounded once.  Y may overlap X.  The workspace holds the
+ * quantised X; the query returns 0 for the few-row problems that do without (ws may be null), unless Y overlaps X: then it is mq_mx_bytes(M, K). */
 size_t mq_mx_linear_workspace_bytes(int M, int N, int K);
 int mq_mx_linear(const void* x, int M, int K, long ldx, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual,
                  long ldr, void* ws, size_t ws_bytes, void* stream);

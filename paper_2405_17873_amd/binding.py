@@ -84,7 +84,9 @@ def _load_native():
         lib = load()
         _mqhost.bind(*(C.cast(getattr(lib, name), C.c_void_p).value for name in (
             "mq_qlinear_w_only", "mq_qlinear_w8a8", "mq_qlinear_w4a8", "mq_qlinear_w2a8", "mq_quantize_weights", "mq_pack_weights",
-            "mq_split_workspace_bytes", "mq_qlinear_a8_workspace_bytes", "mq_packed_bytes")))
+            "mq_split_workspace_bytes", "mq_qlinear_a8_workspace_bytes", "mq_packed_bytes", "mq_mx_bytes", "mq_mx_quantize", "mq_mx_dequantize",
+            "mq_mx_linear_workspace_bytes", "mq_mx_linear", "mq_mx_linear_codes", "mq_mx_linear_grad_workspace_bytes", "mq_mx_linear_grad",
+            "mq_layer_norm", "mq_layer_norm_mx", "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad")))
         _native = _mqhost
     return _native
 
@@ -738,6 +740,9 @@ def alloc_search(sens_content, params_content, sens_quality, params_quality, bit
 # Matrices are [rows, columns] with contiguous rows, which may lie apart.
 
 
+_HALF = (None, torch.float16)  # mx_linear's default
+
+
 @dataclass
 class MxTensor:
     """A [rows, K] matrix in microscaled 4-bit floats, in the product's form.  top: for weights whose layer is differentiated."""
@@ -797,6 +802,9 @@ def _new_mx(rows: int, K: int, device) -> MxTensor:
 
 def mx_quantize(x: torch.Tensor) -> MxTensor:
     """[M, K] fp16/bf16 -> MXFP4: blocks of 32 values of a row, e2m1 codes (nearest, ties to even) times a power of two."""
+    r = (_native or _load_native()).mx_quantize(x)
+    if r is not None:
+        return MxTensor(_done(r, "mq_mx_quantize"), x.shape[0], x.shape[1])
     M, K = _matrix(x).shape
     dt = _dtype_code(x)
     t = _new_mx(M, K, x.device)
@@ -817,6 +825,10 @@ def _with_top(t: MxTensor) -> MxTensor:
 
 def mx_dequantize(t: MxTensor, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values that `t` stands for, rounded to dtype (bfloat16 holds every one)."""
+    if out is None:
+        r = (_native or _load_native()).mx_dequantize(t.data, t.rows, t.K, 0 if dtype == torch.float16 else 1 if dtype == torch.bfloat16 else -1)
+        if r is not None:
+            return _done(r, "mq_mx_dequantize")
     y = _out(out, t.rows, t.K, dtype, t.data.device)
     _check(load().mq_mx_dequantize(_ptr(t.data), t.rows, t.K, _dtype_code(y), _ptr(y), _ld(y), _stream()), "mq_mx_dequantize")
     return y
@@ -850,8 +862,19 @@ def mx_linear(x: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[torc
               residual: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, dtype=None) -> torch.Tensor:
     """Y = mx(X) . W^T + bias (+ residual).  X: [M, K] fp16/bf16, quantised in the call, or an MxTensor; then dtype (fp16 unless out or
     dtype says otherwise) is the output's.  residual may be out itself.  ws: optional uint8 workspace of mx_linear_workspace_bytes(M, N, K)."""
-    lib = load()
     packed = isinstance(x, MxTensor)
+    if out is None and ws is None:
+        native = _native or _load_native()
+        if packed:
+            if x.K == w.K:
+                r = native.mx_linear_codes(x.data, x.rows, x.K, w.data, w.rows, bias, residual, 1 if dtype == torch.bfloat16 else 0 if dtype in _HALF else -1)
+                if r is not None:
+                    return _done(r, "mq_mx_linear_codes")
+        elif dtype is None and w is not None:
+            r = native.mx_linear(x, w.data, w.rows, w.K, bias, residual)
+            if r is not None:
+                return _done(r, "mq_mx_linear")
+    lib = load()
     if packed:
         M, K, device = x.rows, x.K, x.data.device
         dtype = dtype or (out.dtype if out is not None else torch.float16)
@@ -870,7 +893,8 @@ def mx_linear(x: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[torc
     if packed:
         _check(lib.mq_mx_linear_codes(_ptr(x.data), M, K, *args, _stream()), "mq_mx_linear_codes")
     else:
-        ws = _workspace(mx_linear_workspace_bytes(M, w.rows, K), device, ws)
+        if ws is None:  # (a few rows do without, unless the output lies over them)
+            ws = torch.empty(mx_linear_workspace_bytes(M, w.rows, K) if out is None else mx_bytes(M, K), dtype=torch.uint8, device=device)
         _check(lib.mq_mx_linear(_ptr(x), M, K, _ld(x), *args, _ptr(ws), _bytes_of(ws), _stream()), "mq_mx_linear")
     return y
 
@@ -882,9 +906,13 @@ def mx_linear_grad_workspace_bytes(M: int, N: int, K: int) -> int:
 def mx_linear_grad(dy: torch.Tensor, w: MxTensor, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dX = dY . W, the gradient of mx_linear with respect to its input (the quantisation of X passed straight through).  ws: optional uint8
     workspace of mx_linear_grad_workspace_bytes(M, N, K)."""
-    M, N = _matrix(dy, cols=w.rows).shape
     if w.top is None:
         raise ValueError("weights without `top`: make them with mx_quantize_weights or mx_pack")
+    if out is None and ws is None:
+        r = (_native or _load_native()).mx_linear_grad(dy, w.data, w.rows, w.K, w.top)
+        if r is not None:
+            return _done(r, "mq_mx_linear_grad")
+    M, N = _matrix(dy, cols=w.rows).shape
     dx = _out(out, M, w.K, dy.dtype, dy.device)
     ws = _workspace(mx_linear_grad_workspace_bytes(M, N, w.K), dy.device, ws)
     _check(load().mq_mx_linear_grad(_ptr(dy), M, N, _ld(dy), _ptr(w.data), _ptr(w.top), w.K, _ptr(dx), _ld(dx), _dtype_code(dy), *_ws_args(ws),
@@ -911,6 +939,10 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
                out: Optional[torch.Tensor] = None, want_stats: bool = False):
     """Layer norm over the columns of x [M, C] fp16/bf16; weight, bias [C] in 16 bits or float32.  want_stats: (y, mean, rstd), the latter
     two float32 [M], for layer_norm_grad.  out may be x."""
+    if out is None:
+        r = (_native or _load_native()).layer_norm(x, weight, bias, eps, want_stats, False)
+        if r is not None:
+            return _done(r, "mq_layer_norm")
     M, N = _matrix(x).shape
     w, b, pt = _params(x, weight, bias)
     mean, rstd = _stats(x, want_stats)
@@ -923,6 +955,10 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
 def layer_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                   want_stats: bool = False):
     """Layer norm whose output is quantised to MXFP4 from its float32 values: the input of the mx_linear behind it.  C % 32 == 0."""
+    r = (_native or _load_native()).layer_norm(x, weight, bias, eps, want_stats, True)
+    if r is not None:
+        r = _done(r, "mq_layer_norm_mx")
+        return (MxTensor(r[0], *x.shape), r[1], r[2]) if want_stats else MxTensor(r, *x.shape)
     M, N = _matrix(x).shape
     w, b, pt = _params(x, weight, bias)
     mean, rstd = _stats(x, want_stats)
@@ -940,6 +976,10 @@ def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Te
                     residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """(dx, dweight, dbias) of layer_norm and layer_norm_mx; dweight and dbias float32 [C].  residual [M, C]: a gradient that reaches x past the norm,
     added to dx.  out may be dy or residual."""
+    if out is None and ws is None:
+        r = (_native or _load_native()).layer_norm_grad(dy, x, weight, mean, rstd, residual)
+        if r is not None:
+            return _done(r, "mq_layer_norm_grad")
     M, N = _matrix(x).shape
     _matrix(dy, M, N, x.dtype)
     if residual is not None:

@@ -31,7 +31,7 @@ PER_FILE = {
     "norm.hip": ["-fno-slp-vectorize"],
 }
 SOURCES = ["api.hip", "quant_pack.hip", "act_quant.hip", "gemm.hip", "gemm_solo.hip", "gemm_panel.hip", "bos.hip", "prof.hip", "peaks.hip", "alloc.cpp",
-           "mx_quant.hip", "mx_gemm.hip", "mx_grad.hip", "norm.hip", "api_mx.hip"]
+           "mx_quant.hip", "mx_gemm.hip", "mx_rows.hip", "mx_grad.hip", "norm.hip", "api_mx.hip"]
 
 
 def _compile(src: str, force: bool) -> str:

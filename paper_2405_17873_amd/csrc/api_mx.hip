@@ -33,10 +33,8 @@ static int check_product(int M, int N, int K, const void* w, const void* bias, c
     return MQ_OK;
 }
 
-static int product(const void* a, int M, int K, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual, long ldr,
-                   hipStream_t st) {
-    MxGemm g;
-    g.a = mx_view(a, M, K);
+static MxGemm product(int M, int K, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual, long ldr) {
+    MxGemm g = {};
     g.w = mx_view(w, N, K);
     g.M = M;
     g.N = N;
@@ -48,7 +46,11 @@ static int product(const void* a, int M, int K, const void* w, int N, const void
     g.ldr = ldr;
     g.dtype = dtype;
     g.wide = N % 8 == 0 && ldy % 8 == 0 && aligned(y, 16) && (!residual || (ldr % 8 == 0 && aligned(residual, 16))) && aligned(bias, 8);
-    return launch_mx_gemm(g, st);
+    return g;
+}
+static int run(MxGemm& g, const void* a, hipStream_t st) {
+    g.a = mx_view(a, g.M, g.K);
+    return mx_rows_takes(g.M, g.N) ? launch_mx_rows(g, nullptr, 0, st) : launch_mx_gemm(g, st);
 }
 
 static int check_norm(const void* x, int M, int C, long ldx, const void* weight, const void* bias, int param_dtype, int dtype) {
@@ -102,24 +104,32 @@ int mq_mx_column_top(const void* mx, int rows, int K, uint8_t* top, void* stream
     return launch_mx_column_top(mx, rows, K, top, (hipStream_t)stream);
 }
 
-size_t mq_mx_linear_workspace_bytes(int M, int N, int K) { return M <= 0 || N <= 0 || K <= 0 || K % 32 != 0 ? 0 : up256(mx_bytes(M, K)); }
+size_t mq_mx_linear_workspace_bytes(int M, int N, int K) {
+    return M <= 0 || N <= 0 || K <= 0 || K % 32 != 0 || mx_rows_quantizes(M, N, K) ? 0 : up256(mx_bytes(M, K));
+}
 
 int mq_mx_linear(const void* x, int M, int K, long ldx, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual,
                  long ldr, void* ws, size_t ws_bytes, void* stream) {
     int rc;
     if ((rc = check_product(M, N, K, w, bias, y, ldy, dtype, residual, ldr)) || (rc = check_matrix(x, M, ldx, K))) return rc;
     if (M == 0) return MQ_OK;
+    MxGemm g = product(M, K, w, N, bias, y, ldy, dtype, residual, ldr);
+    // (one launch reads activations while others of its workgroups store results)
+    const bool apart = (uintptr_t)y >= (uintptr_t)x + ((size_t)(M - 1) * ldx + K) * 2 || (uintptr_t)x >= (uintptr_t)y + ((size_t)(M - 1) * ldy + N) * 2;
+    if (apart && mx_rows_quantizes(M, N, K)) return launch_mx_rows(g, x, ldx, (hipStream_t)stream);
     if (!ws || !aligned(ws, 256)) return MQ_ERR_BAD_ARG;
-    if (ws_bytes < mq_mx_linear_workspace_bytes(M, N, K)) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    if (ws_bytes < up256(mx_bytes(M, K))) return MQ_ERR_WORKSPACE_TOO_SMALL;
     if ((rc = launch_mx_quantize(x, M, K, ldx, dtype, ws, (hipStream_t)stream))) return rc;
-    return product(ws, M, K, w, N, bias, y, ldy, dtype, residual, ldr, (hipStream_t)stream);
+    return run(g, ws, (hipStream_t)stream);
 }
 
 int mq_mx_linear_codes(const void* a, int M, int K, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual, long ldr,
                        void* stream) {
     int rc;
     if ((rc = check_product(M, N, K, w, bias, y, ldy, dtype, residual, ldr)) || (rc = check_mx(a, M, K))) return rc;
-    return M == 0 ? MQ_OK : product(a, M, K, w, N, bias, y, ldy, dtype, residual, ldr, (hipStream_t)stream);
+    if (M == 0) return MQ_OK;
+    MxGemm g = product(M, K, w, N, bias, y, ldy, dtype, residual, ldr);
+    return run(g, a, (hipStream_t)stream);
 }
 
 size_t mq_mx_linear_grad_workspace_bytes(int M, int N, int K) { return M <= 0 || N <= 0 || K <= 0 || K % 32 != 0 ? 0 : up256(mx_grad_workspace_bytes(M, N, K)); }

@@ -2,7 +2,8 @@
 // tensors, allocates what the call returns, reads the current stream and calls the C entry point, whose address the
 // binding hands over once.  In Python two dozen argument conversions, the allocations and the stream lookup cost 10 us a
 // call, more than the kernels of a small layer run: 4 x 1280 x 1280 weight-only 12.9 -> 7.6 us, 256 x 320 x 320 with run-time
-// ranges 20.0 -> 12.1, quantising and packing the eight linears of a 1280-channel block 190 -> 89.
+// ranges 20.0 -> 12.1, quantising and packing the eight linears of a 1280-channel block 190 -> 89.  Microscaled: 1 x 320 x 1280 15.9 -> 4.9 (with one launch in
+// place of two), 1001 x 1952 quantised and read back 19.4 -> 9.4.
 //
 // Every function takes the ordinary case only, plain tensors on the GPU with the expected sizes and no mode or transform
 // that intercepts operations, and returns None for anything else: the binding then goes its general way, which also
@@ -30,6 +31,18 @@ typedef size_t (*split_bytes_fn)(int, int, int);
 typedef size_t (*a8_bytes_fn)(int, int);
 typedef size_t (*packed_bytes_fn)(int, int, int, int);
 
+typedef size_t (*mx_bytes_fn)(int, int);
+typedef size_t (*mx_ws_fn)(int, int, int);
+typedef int (*mx_quantize_fn)(const void*, int, int, long, int, void*, void*);
+typedef int (*mx_dequantize_fn)(const void*, int, int, int, void*, long, void*);
+typedef int (*mx_linear_fn)(const void*, int, int, long, const void*, int, const void*, void*, long, int, const void*, long, void*, size_t, void*);
+typedef int (*mx_codes_fn)(const void*, int, int, const void*, int, const void*, void*, long, int, const void*, long, void*);
+typedef int (*mx_grad_fn)(const void*, int, int, long, const void*, const uint8_t*, int, void*, long, int, void*, size_t, void*);
+typedef int (*norm_fn)(const void*, int, int, long, const void*, const void*, int, float, void*, long, int, float*, float*, void*);
+typedef int (*norm_mx_fn)(const void*, int, int, long, const void*, const void*, int, float, void*, int, float*, float*, void*);
+typedef int (*norm_grad_fn)(const void*, long, const void*, long, int, int, const void*, int, const float*, const float*, const void*, long, void*, long,
+                            int, float*, float*, void*, size_t, void*);
+
 struct Entry {
     w_only_fn w_only;
     w8a8_fn w8a8;
@@ -39,6 +52,18 @@ struct Entry {
     split_bytes_fn split_bytes;
     a8_bytes_fn a8_bytes;
     packed_bytes_fn packed_bytes;
+    mx_bytes_fn mx_bytes;
+    mx_quantize_fn mx_quantize;
+    mx_dequantize_fn mx_dequantize;
+    mx_ws_fn mx_linear_ws;
+    mx_linear_fn mx_linear;
+    mx_codes_fn mx_codes;
+    mx_ws_fn mx_grad_ws;
+    mx_grad_fn mx_grad;
+    norm_fn norm;
+    norm_mx_fn norm_mx;
+    mx_bytes_fn norm_grad_ws;
+    norm_grad_fn norm_grad;
 } entry;
 
 // An ordinary tensor on the GPU (torch.Tensor or Parameter itself), or nullptr.
@@ -272,14 +297,269 @@ PyObject* pack_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
 }
 
+// ---- microscaled 4-bit floats, layer norm, and their gradients
+
+int dtype_of(at::ScalarType t) { return t == at::kHalf ? 0 : t == at::kBFloat16 ? 1 : -1; }
+
+// A 16-bit matrix on the GPU whose rows are contiguous and do not overlap; its size, row stride and type.
+struct Matrix {
+    const at::Tensor* t;
+    void* p;
+    int rows, cols, dtype;
+    long ld;
+};
+bool matrix(PyObject* o, Matrix& m) {
+    m.t = gpu_tensor(o);
+    if (!m.t || m.t->dim() != 2 || !fits(m.t->size(0)) || !fits(m.t->size(1))) return false;
+    m.rows = (int)m.t->size(0), m.cols = (int)m.t->size(1), m.dtype = dtype_of(m.t->scalar_type());
+    m.ld = m.rows > 1 ? (long)m.t->stride(0) : m.cols;
+    m.p = m.t->data_ptr();
+    return m.dtype >= 0 && m.rows > 0 && m.cols > 0 && (m.cols == 1 || m.t->stride(1) == 1) && m.ld >= m.cols;
+}
+// The same as an optional operand of a given size and type: all zero for None.
+bool optional_matrix(PyObject* o, int rows, int cols, int dtype, Matrix& m) {
+    m = Matrix{};
+    return o == Py_None || (matrix(o, m) && m.rows == rows && m.cols == cols && m.dtype == dtype);
+}
+// An optional contiguous vector of n on x's device (its type in *type).
+bool vector(PyObject* o, int64_t n, at::Device device, void*& p, at::ScalarType* type) {
+    const at::Tensor* t = nullptr;
+    if (!optional_ptr(o, p, &t)) return false;
+    if (!t) return true;
+    if (t->dim() != 1 || t->size(0) != n || (n > 1 && t->stride(0) != 1) || t->device() != device) return false;
+    *type = t->scalar_type();
+    return true;
+}
+// A microscaled buffer of rows x K: its address, or false.
+bool mx_data(PyObject* o, int rows, int K, void*& p) {
+    const at::Tensor* t = gpu_tensor(o);
+    if (!t || rows <= 0 || K <= 0 || t->scalar_type() != at::kByte || t->nbytes() < entry.mx_bytes(rows, K)) return false;
+    p = t->data_ptr();
+    return true;
+}
+at::Tensor workspace(size_t bytes, at::Device device) { return empty({(int64_t)bytes}, at::kByte, device); }
+PyObject* pair_or_more(std::initializer_list<at::Tensor> list) {
+    PyObject* t = PyTuple_New((Py_ssize_t)list.size());
+    Py_ssize_t i = 0;
+    for (const at::Tensor& v : list) {
+        PyObject* o = t ? THPVariable_Wrap(v) : nullptr;
+        if (!o) {
+            Py_XDECREF(t);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(t, i++, o);
+    }
+    return t;
+}
+
+// (x) -> data, code or None
+PyObject* mx_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix x;
+        if (n != 1 || !plain_calls() || !matrix(a[0], x) || x.cols % 32 != 0) return general();
+        at::Tensor data;
+        int rc;
+        {
+            Unlocked unlocked;
+            data = workspace(entry.mx_bytes(x.rows, x.cols), x.t->device());
+            rc = entry.mx_quantize(x.p, x.rows, x.cols, x.ld, x.dtype, data.data_ptr(), stream());
+        }
+        return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(std::move(data));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// (data, rows, K, dtype) -> matrix, code or None
+PyObject* mx_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        int rows, K, dtype;
+        void* p;
+        if (n != 4 || !plain_calls() || !small_int(a[1], rows) || !small_int(a[2], K) || !small_int(a[3], dtype) || (dtype != 0 && dtype != 1) ||
+            !mx_data(a[0], rows, K, p))
+            return general();
+        const at::Device device = gpu_tensor(a[0])->device();
+        at::Tensor y;
+        int rc;
+        {
+            Unlocked unlocked;
+            y = empty({rows, K}, dtype ? at::kBFloat16 : at::kHalf, device);
+            rc = entry.mx_dequantize(p, rows, K, dtype, y.data_ptr(), K, stream());
+        }
+        return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(std::move(y));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// (x, w, N, K, bias, residual) -> y, code or None: the output and the workspace are allocated here
+PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix x, res;
+        int N, K;
+        void *w, *bias;
+        if (n != 6 || !plain_calls() || !matrix(a[0], x) || !small_int(a[2], N) || !small_int(a[3], K) || x.cols != K || !mx_data(a[1], N, K, w))
+            return general();
+        const at::Device device = x.t->device();
+        at::ScalarType type = x.t->scalar_type();
+        if (!vector(a[4], N, device, bias, &type) || type != x.t->scalar_type() || !optional_matrix(a[5], x.rows, N, x.dtype, res)) return general();
+        at::Tensor y, ws;
+        int rc;
+        {
+            Unlocked unlocked;
+            y = empty({x.rows, N}, type, device);
+            const size_t need = entry.mx_linear_ws(x.rows, N, K);
+            if (need) ws = workspace(need, device);
+            rc = entry.mx_linear(x.p, x.rows, K, x.ld, w, N, bias, y.data_ptr(), N, x.dtype, res.p, res.ld, need ? ws.data_ptr() : nullptr, need, stream());
+        }
+        return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(std::move(y));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// (data, M, K, w, N, bias, residual, dtype) -> y, code or None
+PyObject* mx_linear_codes(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix res;
+        int M, K, N, dtype;
+        void *x, *w, *bias;
+        if (n != 8 || !plain_calls() || !small_int(a[1], M) || !small_int(a[2], K) || !small_int(a[4], N) || !small_int(a[7], dtype) ||
+            (dtype != 0 && dtype != 1) || !mx_data(a[0], M, K, x) || !mx_data(a[3], N, K, w))
+            return general();
+        const at::Device device = gpu_tensor(a[0])->device();
+        const at::ScalarType want = dtype ? at::kBFloat16 : at::kHalf;
+        at::ScalarType type = want;
+        if (!vector(a[5], N, device, bias, &type) || type != want || !optional_matrix(a[6], M, N, dtype, res)) return general();
+        at::Tensor y;
+        int rc;
+        {
+            Unlocked unlocked;
+            y = empty({M, N}, want, device);
+            rc = entry.mx_codes(x, M, K, w, N, bias, y.data_ptr(), N, dtype, res.p, res.ld, stream());
+        }
+        return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(std::move(y));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// (dy, w, N, K, top) -> dx, code or None
+PyObject* mx_linear_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix dy;
+        int N, K;
+        void* w;
+        const at::Tensor* top;
+        if (n != 5 || !plain_calls() || !matrix(a[0], dy) || !small_int(a[2], N) || !small_int(a[3], K) || dy.cols != N || !mx_data(a[1], N, K, w) ||
+            !(top = gpu_tensor(a[4])) || top->scalar_type() != at::kByte || !top->is_contiguous() || top->numel() != K / 32)
+            return general();
+        const void* tp = top->data_ptr();
+        const at::Device device = dy.t->device();
+        at::Tensor dx, ws;
+        int rc;
+        {
+            Unlocked unlocked;
+            dx = empty({dy.rows, K}, dy.t->scalar_type(), device);
+            const size_t need = entry.mx_grad_ws(dy.rows, N, K);
+            if (need) ws = workspace(need, device);
+            rc = entry.mx_grad(dy.p, dy.rows, N, dy.ld, w, (const uint8_t*)tp, K, dx.data_ptr(), K, dy.dtype, need ? ws.data_ptr() : nullptr, need, stream());
+        }
+        return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(std::move(dx));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// Weight and bias of a norm over x's columns: addresses and type number.
+bool norm_params(PyObject* weight, PyObject* bias, const Matrix& x, void*& w, void*& b, int& type) {
+    at::ScalarType tw = at::kFloat, tb = at::kFloat;
+    if (!vector(weight, x.cols, x.t->device(), w, &tw) || !vector(bias, x.cols, x.t->device(), b, &tb) || (w && b && tw != tb)) return false;
+    const at::ScalarType t = w ? tw : tb;
+    type = t == at::kFloat ? 2 : dtype_of(t);
+    return type >= 0;
+}
+bool flag(PyObject* o, bool& v) {
+    if (!PyBool_Check(o)) return false;
+    v = o == Py_True;
+    return true;
+}
+
+// (x, weight, bias, eps, want_stats, mx) -> y or data, or (it, mean, rstd); code or None
+PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix x;
+        void *w, *b;
+        int pt;
+        bool stats, mx;
+        if (n != 6 || !plain_calls() || !matrix(a[0], x) || !norm_params(a[1], a[2], x, w, b, pt) || !PyFloat_CheckExact(a[3]) || !flag(a[4], stats) ||
+            !flag(a[5], mx) || (mx && x.cols % 32 != 0))
+            return general();
+        const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
+        const at::Device device = x.t->device();
+        at::Tensor y, mean, rstd;
+        int rc;
+        {
+            Unlocked unlocked;
+            y = mx ? workspace(entry.mx_bytes(x.rows, x.cols), device) : empty({x.rows, x.cols}, x.t->scalar_type(), device);
+            if (stats) mean = empty({x.rows}, at::kFloat, device), rstd = empty({x.rows}, at::kFloat, device);
+            float *mp = stats ? (float*)mean.data_ptr() : nullptr, *rp = stats ? (float*)rstd.data_ptr() : nullptr;
+            rc = mx ? entry.norm_mx(x.p, x.rows, x.cols, x.ld, w, b, pt, eps, y.data_ptr(), x.dtype, mp, rp, stream())
+                    : entry.norm(x.p, x.rows, x.cols, x.ld, w, b, pt, eps, y.data_ptr(), x.cols, x.dtype, mp, rp, stream());
+        }
+        if (rc) return PyLong_FromLong(rc);
+        return stats ? pair_or_more({y, mean, rstd}) : THPVariable_Wrap(std::move(y));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// (dy, x, weight, mean, rstd, residual) -> (dx, dweight, dbias), code or None
+PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix dy, x, res;
+        void *w, *b, *mean, *rstd;
+        int pt;
+        at::ScalarType tm = at::kFloat, tr = at::kFloat;
+        if (n != 6 || !plain_calls() || !matrix(a[1], x) || !matrix(a[0], dy) || dy.rows != x.rows || dy.cols != x.cols || dy.dtype != x.dtype ||
+            !norm_params(a[2], Py_None, x, w, b, pt) || !vector(a[3], x.rows, x.t->device(), mean, &tm) ||
+            !vector(a[4], x.rows, x.t->device(), rstd, &tr) || !mean || !rstd || tm != at::kFloat || tr != at::kFloat ||
+            !optional_matrix(a[5], x.rows, x.cols, x.dtype, res))
+            return general();
+        const at::Device device = x.t->device();
+        at::Tensor dx, dw, db, ws;
+        int rc;
+        {
+            Unlocked unlocked;
+            dx = empty({x.rows, x.cols}, x.t->scalar_type(), device);
+            dw = empty({x.cols}, at::kFloat, device), db = empty({x.cols}, at::kFloat, device);
+            const size_t need = entry.norm_grad_ws(x.rows, x.cols);
+            ws = workspace(need, device);
+            rc = entry.norm_grad(dy.p, dy.ld, x.p, x.ld, x.rows, x.cols, w, pt, (const float*)mean, (const float*)rstd, res.p, res.ld, dx.data_ptr(), x.cols,
+                                 x.dtype, (float*)dw.data_ptr(), (float*)db.data_ptr(), ws.data_ptr(), need, stream());
+        }
+        return rc ? PyLong_FromLong(rc) : pair_or_more({dx, dw, db});
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
 // Addresses of the C entry points, in the order of Entry.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    void* p[9];
-    if (n != 9) {
-        PyErr_SetString(PyExc_TypeError, "bind takes nine addresses");
+    constexpr int COUNT = sizeof(Entry) / sizeof(void*);
+    void* p[COUNT];
+    if (n != COUNT) {
+        PyErr_SetString(PyExc_TypeError, "bind takes the address of every entry point");
         return nullptr;
     }
-    for (int i = 0; i < 9; ++i) {
+    for (int i = 0; i < COUNT; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null entry point");
@@ -287,7 +567,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
     }
     entry = Entry{(w_only_fn)p[0], (w8a8_fn)p[1], (wxa8_fn)p[2], (wxa8_fn)p[3], (quantize_fn)p[4], (pack_fn)p[5], (split_bytes_fn)p[6],
-                  (a8_bytes_fn)p[7], (packed_bytes_fn)p[8]};
+                  (a8_bytes_fn)p[7], (packed_bytes_fn)p[8], (mx_bytes_fn)p[9], (mx_quantize_fn)p[10], (mx_dequantize_fn)p[11], (mx_ws_fn)p[12],
+                  (mx_linear_fn)p[13], (mx_codes_fn)p[14], (mx_ws_fn)p[15], (mx_grad_fn)p[16], (norm_fn)p[17], (norm_mx_fn)p[18],
+                  (mx_bytes_fn)p[19], (norm_grad_fn)p[20]};
     Py_RETURN_NONE;
 }
 
@@ -297,6 +579,13 @@ PyMethodDef methods[] = {
     {"qlinear_a8", (PyCFunction)(void (*)(void))qlinear_a8, METH_FASTCALL, nullptr},
     {"quantize_weights", (PyCFunction)(void (*)(void))quantize_weights, METH_FASTCALL, nullptr},
     {"pack_weights", (PyCFunction)(void (*)(void))pack_weights, METH_FASTCALL, nullptr},
+    {"mx_quantize", (PyCFunction)(void (*)(void))mx_quantize, METH_FASTCALL, nullptr},
+    {"mx_dequantize", (PyCFunction)(void (*)(void))mx_dequantize, METH_FASTCALL, nullptr},
+    {"mx_linear", (PyCFunction)(void (*)(void))mx_linear, METH_FASTCALL, nullptr},
+    {"mx_linear_codes", (PyCFunction)(void (*)(void))mx_linear_codes, METH_FASTCALL, nullptr},
+    {"mx_linear_grad", (PyCFunction)(void (*)(void))mx_linear_grad, METH_FASTCALL, nullptr},
+    {"layer_norm", (PyCFunction)(void (*)(void))layer_norm, METH_FASTCALL, nullptr},
+    {"layer_norm_grad", (PyCFunction)(void (*)(void))layer_norm_grad, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mqhost", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -149,6 +149,9 @@ int launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int M, int K, vo
 int launch_mx_unpack(const void* mx, int M, int K, uint8_t* codes, uint8_t* scales, hipStream_t st);
 int launch_mx_column_top(const void* mx, int rows, int K, uint8_t* top, hipStream_t st);
 int launch_mx_gemm(const MxGemm& g, hipStream_t st);
+int launch_mx_rows(const MxGemm& g, const void* x, long ldx, hipStream_t st);  // x: 16-bit activations, or null: g.a
+bool mx_rows_takes(int M, int N);
+bool mx_rows_quantizes(int M, int N, int K);
 int launch_mx_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* ws,
                    hipStream_t st);
 size_t mx_grad_workspace_bytes(long M, long N, long K);

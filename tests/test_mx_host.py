@@ -93,7 +93,8 @@ def test_sizes(lib):
     assert mq.mx_bytes(33, 96) == 2 * 2 * 1024 + 2 * 256
     assert mq.mx_bytes(1, 320) == 5 * 1024 + 2 * 256
     assert mq.mx_bytes(4, 48) == 0 and mq.mx_bytes(-1, 64) == 0 and mq.mx_bytes(0, 64) == 0
-    assert mq.mx_linear_workspace_bytes(4, 8, 64) >= mq.mx_bytes(4, 64)
+    assert mq.mx_linear_workspace_bytes(4, 8, 64) == 0  # a few rows are quantised in the product
+    assert mq.mx_linear_workspace_bytes(64, 8, 64) >= mq.mx_bytes(64, 64)
     assert mq.mx_linear_workspace_bytes(0, 8, 64) == 0
     assert mq.layer_norm_grad_workspace_bytes(1, 8) >= 64 and mq.layer_norm_grad_workspace_bytes(0, 8) == 0
 
@@ -114,7 +115,10 @@ def test_error_codes_without_a_gpu(lib):
     assert lib.mq_mx_column_top(p, 4, 64, null, st) == -1 and lib.mq_mx_column_top(p, 4, 72, p, st) == -2
     lin = lambda x=p, M=4, K=64, ldx=64, w=p, N=8, b=null, y=p, ldy=8, dt=0, r=null, ldr=0, ws=p, wsb=4096: lib.mq_mx_linear(
         x, M, K, L(ldx), w, N, b, y, L(ldy), dt, r, L(ldr), ws, C.c_size_t(wsb), st)
-    assert lin(x=null) == -1 and lin(w=null) == -1 and lin(w=off) == -1 and lin(y=null) == -1 and lin(ws=null) == -1 and lin(ws=off) == -1
+    far = C.c_void_p(p.value + (1 << 30))
+    assert lin(x=null) == -1 and lin(w=null) == -1 and lin(w=off) == -1 and lin(y=null) == -1
+    assert lin(ws=null) == -1 and lin(ws=off) == -1                     # (Y overlaps X)
+    assert lin(M=64, y=far, ws=null) == -1 and lin(M=64, y=far, ws=off) == -1
     assert lin(dt=2) == -1 and lin(b=odd) == -1 and lin(r=odd, ldr=8) == -1
     assert lin(M=-1) == -2 and lin(N=0) == -2 and lin(K=33) == -2 and lin(ldx=32) == -2 and lin(ldy=7) == -2 and lin(r=p, ldr=7) == -2
     assert lin(N=(1 << 22) + 1, ldy=1 << 23) == -2
