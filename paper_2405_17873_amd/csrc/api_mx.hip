@@ -45,7 +45,6 @@ static MxGemm product(int M, int K, const void* w, int N, const void* bias, void
     g.res = (const uint16_t*)residual;
     g.ldr = ldr;
     g.dtype = dtype;
-    g.wide = N % 8 == 0 && ldy % 8 == 0 && aligned(y, 16) && (!residual || (ldr % 8 == 0 && aligned(residual, 16))) && aligned(bias, 8);
     return g;
 }
 static int run(MxGemm& g, const void* a, hipStream_t st) {

@@ -108,10 +108,11 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
     return v > o ? v : o;
 }
 
-// Eight consecutive 16-bit values of a row, of which the first `n` exist (n >= 8: all); `wide`: the address is 16-byte aligned.
-__device__ __forceinline__ uint4v load8_16(const uint16_t* p, int n, bool wide) {
+// Eight consecutive 16-bit values of a row, of which the first `n` exist (n >= 8: all), wherever they start: the memory takes 16 bytes at any address.
+typedef uint4v uint4v_any __attribute__((aligned(2)));
+__device__ __forceinline__ uint4v load8_16(const uint16_t* p, int n) {
     uint4v r = {0, 0, 0, 0};
-    if (wide && n >= 8) return *(const uint4v*)p;
+    if (n >= 8) return *(const uint4v_any*)p;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t lo = 2 * i < n ? p[2 * i] : 0, hi = 2 * i + 1 < n ? p[2 * i + 1] : 0;
@@ -119,9 +120,9 @@ __device__ __forceinline__ uint4v load8_16(const uint16_t* p, int n, bool wide) 
     }
     return r;
 }
-__device__ __forceinline__ void store8_16(uint16_t* p, uint4v v, int n, bool wide) {
-    if (wide && n >= 8) {
-        *(uint4v*)p = v;
+__device__ __forceinline__ void store8_16(uint16_t* p, uint4v v, int n) {
+    if (n >= 8) {
+        *(uint4v_any*)p = v;
         return;
     }
 #pragma unroll
@@ -141,7 +142,6 @@ struct MxGemm {
     const uint16_t* res;
     long ldr;
     int dtype;
-    bool wide;  // rows of y (and of the residual) start on 16-byte boundaries, N % 8 == 0
 };
 int launch_mx_quantize(const void* x, int M, int K, long ldx, int dtype, void* mx, hipStream_t st);
 int launch_mx_dequantize(const void* mx, int M, int K, int dtype, void* y, long ldy, hipStream_t st);

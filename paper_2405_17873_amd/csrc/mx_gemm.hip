@@ -4,6 +4,7 @@
 namespace mq {
 
 typedef int int8v __attribute__((ext_vector_type(8)));
+typedef uint2v uint2v_any __attribute__((aligned(2)));
 
 // One 32 x 32 x 64 step; S: the byte of the scale words that belongs to it.
 template <int S>
@@ -13,10 +14,10 @@ __device__ __forceinline__ float16v mx_mfma(int4v w, int4v a, float16v c, int sw
 }
 
 // The weights are the MFMA's row operand: a lane then holds, of one row of Y, four runs of four consecutive columns (8 t + 4 h, h the lane's half).
-// Where rows are wide (16-byte aligned, N % 8 == 0), two such runs trade places with those of the other half, and the lane has eight consecutive
-// columns, one 16-byte store.  (A kernel has one of the three forms: all of them unrolled over the blocks of a large tile are more code than the
-// instruction cache holds, which a workgroup runs through once; 8 us of a 256 x 256 tile.)
-enum { MX_NARROW, MX_WIDE, MX_WIDE_RES };
+// Two such runs trade places with those of the other half, and the lane has eight consecutive columns; another trade, between the 16 lanes of a row of
+// lanes and the next, and four lanes have the 32 columns of a row, one 64-byte piece.  (A kernel has one of the forms: all of them unrolled over the
+// blocks of a large tile are more code than the instruction cache holds, which a workgroup runs through once; 8 us of a 256 x 256 tile.)
+enum { MX_PLAIN, MX_RES, MX_ODD };  // without a residual; with one; N no multiple of eight, with or without
 // Lanes 16 .. 31 of v[0] and lanes 0 .. 15 of v[1] trade places, likewise in the upper half.  Its own inverse.
 __device__ __forceinline__ void mx_swap16(uint4v* v) {
 #pragma unroll
@@ -28,68 +29,50 @@ __device__ __forceinline__ void mx_swap16(uint4v* v) {
 }
 template <int DT, int EPI>
 __device__ __forceinline__ void mx_store_block(const MxGemm& g, const float16v& acc, const float* bias, long m0, int n0, int lane) {
-    const int h = lane >> 5;
-    if constexpr (EPI != MX_NARROW) {
-        const int q = (lane >> 4) & 1;
-        const int n = n0 + 16 * q + 8 * h;
-        const long m = m0 + (lane & 15);
-        const bool on[2] = {m < g.M && n < g.N, m + 16 < g.M && n < g.N};
-        uint4v v[2];
-        if constexpr (EPI == MX_WIDE_RES) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) v[t] = on[t] ? *(const uint4v*)(g.res + (m + 16 * t) * g.ldr + n) : uint4v{0, 0, 0, 0};
-            mx_swap16(v);
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            float f[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = acc[8 * t + i] + bias[8 * t + i];
-            if constexpr (EPI == MX_WIDE_RES) {
-                const auto p = __builtin_amdgcn_permlane32_swap(v[t][0], v[t][2], false, false), r = __builtin_amdgcn_permlane32_swap(v[t][1], v[t][3], false, false);
-                const uint32_t o[4] = {(uint32_t)p[0], (uint32_t)r[0], (uint32_t)p[1], (uint32_t)r[1]};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] += T16<DT>::up((uint16_t)(o[i >> 1] >> (16 * (i & 1))));
-            }
-            const uint32_t a0 = T16<DT>::pack(f[0], f[1]), a1 = T16<DT>::pack(f[2], f[3]), b0 = T16<DT>::pack(f[4], f[5]), b1 = T16<DT>::pack(f[6], f[7]);
-            const auto p = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), r = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
-            v[t] = uint4v{(uint32_t)p[0], (uint32_t)r[0], (uint32_t)p[1], (uint32_t)r[1]};
-        }
-        mx_swap16(v);
+    const int h = lane >> 5, q = (lane >> 4) & 1;
+    const int n = n0 + 16 * q + 8 * h, left = g.N - n;
+    const long m = m0 + (lane & 15);
+    const bool on[2] = {m < g.M && left > 0, m + 16 < g.M && left > 0};
+    uint4v v[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (EPI == MX_RES || (EPI == MX_ODD && g.res)) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-            if (on[t]) *(uint4v*)(g.y + (m + 16 * t) * g.ldy + n) = v[t];
-    } else {
-        const long m = m0 + (lane & 31);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int n = n0 + 8 * (i >> 2) + 4 * h + (i & 3);
-            if (m < g.M && n < g.N) {
-                float f = acc[i] + bias[i];
-                if (g.res) f += T16<DT>::up(g.res[m * g.ldr + n]);
-                g.y[m * g.ldy + n] = T16<DT>::down(f);
-            }
-        }
+            if (on[t]) v[t] = load8_16(g.res + (m + 16 * t) * g.ldr + n, EPI == MX_ODD ? left : 8);
+        mx_swap16(v);
     }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = acc[8 * t + i] + bias[8 * t + i];
+        if (EPI == MX_RES || (EPI == MX_ODD && g.res)) {
+            const auto p = __builtin_amdgcn_permlane32_swap(v[t][0], v[t][2], false, false), r = __builtin_amdgcn_permlane32_swap(v[t][1], v[t][3], false, false);
+            const uint32_t o[4] = {(uint32_t)p[0], (uint32_t)r[0], (uint32_t)p[1], (uint32_t)r[1]};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] += T16<DT>::up((uint16_t)(o[i >> 1] >> (16 * (i & 1))));
+        }
+        const uint32_t a0 = T16<DT>::pack(f[0], f[1]), a1 = T16<DT>::pack(f[2], f[3]), b0 = T16<DT>::pack(f[4], f[5]), b1 = T16<DT>::pack(f[6], f[7]);
+        const auto p = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), r = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+        v[t] = uint4v{(uint32_t)p[0], (uint32_t)r[0], (uint32_t)p[1], (uint32_t)r[1]};
+    }
+    mx_swap16(v);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+        if (on[t]) store8_16(g.y + (m + 16 * t) * g.ldy + n, v[t], EPI == MX_ODD ? left : 8);
 }
 
 // Bias of a block's columns, in the accumulators' order.
 template <int DT, int EPI>
 __device__ __forceinline__ void mx_bias_block(const MxGemm& g, int n0, int h, float* c) {
-    if constexpr (EPI != MX_NARROW) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int n = n0 + 8 * t + 4 * h;
-            uint2v b = {0, 0};
-            if (g.bias && n < g.N) b = *(const uint2v*)(g.bias + n);
+    for (int t = 0; t < 4; ++t) {
+        const int n = n0 + 8 * t + 4 * h;
+        uint2v b = {0, 0};
+        if (g.bias && (EPI == MX_ODD ? n + 4 <= g.N : n < g.N)) b = *(const uint2v_any*)(g.bias + n);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) c[4 * t + i] = T16<DT>::up((uint16_t)(b[i >> 1] >> (16 * (i & 1))));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int n = n0 + 8 * (i >> 2) + 4 * h + (i & 3);
-            c[i] = g.bias && n < g.N ? T16<DT>::up(g.bias[n]) : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            c[4 * t + i] = T16<DT>::up((uint16_t)(b[i >> 1] >> (16 * (i & 1))));
+            if (EPI == MX_ODD && g.bias && n + 4 > g.N && n + i < g.N) c[4 * t + i] = T16<DT>::up(g.bias[n + i]);
         }
     }
 }
@@ -296,8 +279,8 @@ static int run_mx_form(const MxGemm& g, long band, hipStream_t st) {
 
 template <int DT, int WM, int WN, int TM, int TN, int S>
 static int run_mx_gemm(const MxGemm& g, long band, hipStream_t st) {
-    if (!g.wide) return run_mx_form<DT, MX_NARROW, 2, 2, 2, 2, 4>(g, band, st);
-    return g.res ? run_mx_form<DT, MX_WIDE_RES, WM, WN, TM, TN, S>(g, band, st) : run_mx_form<DT, MX_WIDE, WM, WN, TM, TN, S>(g, band, st);
+    if (g.N % 8 != 0) return run_mx_form<DT, MX_ODD, 2, 2, 2, 2, 4>(g, band, st);
+    return g.res ? run_mx_form<DT, MX_RES, WM, WN, TM, TN, S>(g, band, st) : run_mx_form<DT, MX_PLAIN, WM, WN, TM, TN, S>(g, band, st);
 }
 
 // 256 x 256 tiles with two waves per SIMD, or 128 x 128 with one and up to three workgroups per compute unit.  The large tile moves half as much per

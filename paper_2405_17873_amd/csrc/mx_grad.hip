@@ -22,7 +22,7 @@ struct MxGrad {
     int M, N, K;
     uint16_t* dx;
     long lddx;
-    bool wide_in, wide_out;
+    bool wide;  // rows of dY start on 16-byte boundaries
 };
 
 // Exponent field that a block with the largest scale of its column is widened with: 6 units are then 49152 in fp16, 1.5 in bfloat16.
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
                     b += *(const lds_float4v*)(uintptr_t)(at + 16);
                 }
                 if (whole) {
-                    store8_16(g.dx + mm * g.lddx + k, mx_grad_result<DT>(a, b, (int)g.top[k >> 5]), 8, g.wide_out);
+                    store8_16(g.dx + mm * g.lddx + k, mx_grad_result<DT>(a, b, (int)g.top[k >> 5]), 8);
                 } else {
                     float* out = work.partial + ((long)(blockIdx.x - work.whole) * (TM * 32) + m * 32 + row) * (TK * 32) + c * 8;
                     *(float4v*)out = a;
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(256) void mx_grad_join_kernel(const MxGrad g, const
         a += *(const float4v*)p;
         b += *(const float4v*)(p + 4);
     }
-    store8_16(g.dx + m * g.lddx + k, mx_grad_result<DT>(a, b, (int)g.top[k >> 5]), 8, g.wide_out);
+    store8_16(g.dx + m * g.lddx + k, mx_grad_result<DT>(a, b, (int)g.top[k >> 5]), 8);
 }
 
 // Any alignment of dY's rows, any N, weights of any size: 64 x 64 results per workgroup, operands through registers.
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(256) void mx_grad_any_kernel(const MxGrad g) {
             const int t = i * 256 + tid, r = t >> 3, p = t & 7;
             const int n = n0 + p * 8;
             uint4v v = {0, 0, 0, 0};
-            if (m0 + r < g.M && n < g.N) v = load8_16(g.dy + (m0 + r) * g.lddy + n, g.N - n, g.wide_in);
+            if (m0 + r < g.M && n < g.N) v = load8_16(g.dy + (m0 + r) * g.lddy + n, g.N - n);
             *(uint4v*)(dt + r * (BN * 2) + ((p ^ (r & 7)) << 4)) = v;
         }
         __syncthreads();
@@ -445,7 +445,7 @@ template <int DT>
 static int choose_mx_grad(const MxGrad& g, float* ws, hipStream_t st) {
     // 32-bit offsets of the loads: a row strip of dY, the weights' codes
     const bool small = g.lddy < (1 << 22) && (long)g.w.groups * g.w.kc * 1024 < (1L << 31);
-    if (!g.wide_in || g.N % 8 != 0 || !small) {
+    if (!g.wide || g.N % 8 != 0 || !small) {
         mx_grad_any_kernel<DT><<<dim3((unsigned)((g.M + 63L) / 64), (unsigned)g.w.kc), 256, 0, st>>>(g);
         MQ_HIP_CHECK_LAUNCH();
         return MQ_OK;
@@ -466,8 +466,7 @@ int launch_mx_grad(const void* dy, int M, int N, long lddy, const void* w, const
     g.K = K;
     g.dx = (uint16_t*)dx;
     g.lddx = lddx;
-    g.wide_in = (M == 1 || g.lddy % 8 == 0) && (uintptr_t)dy % 16 == 0;
-    g.wide_out = (M == 1 || lddx % 8 == 0) && (uintptr_t)dx % 16 == 0;
+    g.wide = (M == 1 || g.lddy % 8 == 0) && (uintptr_t)dy % 16 == 0;
     return dtype == MQ_F16 ? choose_mx_grad<MQ_F16>(g, (float*)ws, st) : choose_mx_grad<MQ_BF16>(g, (float*)ws, st);
 }
 

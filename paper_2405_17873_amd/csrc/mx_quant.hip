@@ -7,7 +7,7 @@ namespace mq {
 // whole 128-byte pieces of eight rows and writes two of 128 bytes (8 neighbouring rows of one block column).  Four such steps, 256 columns, make the
 // scale word of a row and block column.  Bound by memory: 2 bytes read and 17/32 written per value.
 template <int DT>
-__global__ __launch_bounds__(256) void mx_quantize_kernel(const uint16_t* x, int M, int K, long ldx, bool wide, uint8_t* codes, uint8_t* scales,
+__global__ __launch_bounds__(256) void mx_quantize_kernel(const uint16_t* x, int M, int K, long ldx, uint8_t* codes, uint8_t* scales,
                                                           int kc, int kq) {
     const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
     const int g = blockIdx.y + blockIdx.z * 65535;  // group of 32 rows; a wave takes eight of them
@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const uint16_t* x, int
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const bool in = row < M && k0 + 64 * i < K;  // K % 32 == 0: a block is whole or absent
-        v[i] = in ? load8_16(p + 64 * i, 8, wide) : uint4v{0, 0, 0, 0};
+        v[i] = in ? load8_16(p + 64 * i, 8) : uint4v{0, 0, 0, 0};
     }
     uint32_t word = 0;
     uint8_t* tile = codes + ((long)g * kc + q * 4) * 1024 + (kb * 32 + j) * 16 + part * 4;
@@ -43,13 +43,12 @@ static dim3 rows_grid(int x, long groups) {
 
 int launch_mx_quantize(const void* x, int M, int K, long ldx, int dtype, void* mx, hipStream_t st) {
     const MxView v = mx_view(mx, M, K);
-    const bool wide = ldx % 8 == 0 && (uintptr_t)x % 16 == 0;
     const dim3 grid = rows_grid(v.kq, v.groups);
     uint8_t *codes = (uint8_t*)v.codes, *scales = (uint8_t*)v.scales;
     if (dtype == MQ_F16)
-        mx_quantize_kernel<MQ_F16><<<grid, 256, 0, st>>>((const uint16_t*)x, M, K, ldx, wide, codes, scales, v.kc, v.kq);
+        mx_quantize_kernel<MQ_F16><<<grid, 256, 0, st>>>((const uint16_t*)x, M, K, ldx, codes, scales, v.kc, v.kq);
     else
-        mx_quantize_kernel<MQ_BF16><<<grid, 256, 0, st>>>((const uint16_t*)x, M, K, ldx, wide, codes, scales, v.kc, v.kq);
+        mx_quantize_kernel<MQ_BF16><<<grid, 256, 0, st>>>((const uint16_t*)x, M, K, ldx, codes, scales, v.kc, v.kq);
     MQ_HIP_CHECK_LAUNCH();
     return MQ_OK;
 }
@@ -57,7 +56,7 @@ int launch_mx_quantize(const void* x, int M, int K, long ldx, int dtype, void* m
 // The way back, in the same order of lanes: exact in both types except where the value leaves the range of fp16.
 template <int DT>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int M, int K, int kc, int kq, uint16_t* y,
-                                                            long ldy, bool wide) {
+                                                            long ldy) {
     const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
     const int g = blockIdx.y + blockIdx.z * 65535, q = blockIdx.x;
     if ((long)g * 32 >= M) return;
@@ -86,18 +85,17 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* codes
             o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 2));
             o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 3));
         }
-        store8_16(y + row * ldy + k0 + 64 * i, o, 8, wide);
+        store8_16(y + row * ldy + k0 + 64 * i, o, 8);
     }
 }
 
 int launch_mx_dequantize(const void* mx, int M, int K, int dtype, void* y, long ldy, hipStream_t st) {
     const MxView v = mx_view(mx, M, K);
-    const bool wide = ldy % 8 == 0 && (uintptr_t)y % 16 == 0;
     const dim3 grid = rows_grid(v.kq, v.groups);
     if (dtype == MQ_F16)
-        mx_dequantize_kernel<MQ_F16><<<grid, 256, 0, st>>>(v.codes, v.scales, M, K, v.kc, v.kq, (uint16_t*)y, ldy, wide);
+        mx_dequantize_kernel<MQ_F16><<<grid, 256, 0, st>>>(v.codes, v.scales, M, K, v.kc, v.kq, (uint16_t*)y, ldy);
     else
-        mx_dequantize_kernel<MQ_BF16><<<grid, 256, 0, st>>>(v.codes, v.scales, M, K, v.kc, v.kq, (uint16_t*)y, ldy, wide);
+        mx_dequantize_kernel<MQ_BF16><<<grid, 256, 0, st>>>(v.codes, v.scales, M, K, v.kc, v.kq, (uint16_t*)y, ldy);
     MQ_HIP_CHECK_LAUNCH();
     return MQ_OK;
 }

@@ -13,7 +13,6 @@ struct MxRows {
     MxGemm g;
     const uint16_t* x;  // 16-bit activations, or null: g.a
     long ldx;
-    bool xwide;
 };
 
 template <int DT, bool MXIN, int RG, int U>
@@ -66,7 +65,7 @@ __global__ __launch_bounds__(512, 1) void mx_rows_kernel(const MxRows r) {
                     const bool in = m * 32 + j < g.M && c + u < c1 && k < g.K;
                     const uint16_t* p = r.x + (m * 32 + j) * r.ldx + k;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[u][m][i] = in ? load8_16(p + i * 8, 8, r.xwide) : uint4v{0, 0, 0, 0};
+                    for (int i = 0; i < 4; ++i) v[u][m][i] = in ? load8_16(p + i * 8, 8) : uint4v{0, 0, 0, 0};
                 }
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -121,19 +120,18 @@ __global__ __launch_bounds__(512, 1) void mx_rows_kernel(const MxRows r) {
             for (int e = 0; e < 4; ++e) f[e] += lo[e], f[4 + e] += hi[e];
         }
         if (g.bias) {
-            const uint4v b = load8_16(g.bias + n, left, ((uintptr_t)g.bias & 15) == 0);
+            const uint4v b = load8_16(g.bias + n, left);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] += T16<DT>::up((uint16_t)(b[e >> 1] >> (16 * (e & 1))));
         }
         if (g.res) {
             const uint16_t* p = g.res + m * g.ldr + n;
-            const uint4v b = load8_16(p, left, ((uintptr_t)p & 15) == 0);
+            const uint4v b = load8_16(p, left);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] += T16<DT>::up((uint16_t)(b[e >> 1] >> (16 * (e & 1))));
         }
         uint16_t* y = g.y + m * g.ldy + n;
-        store8_16(y, uint4v{T16<DT>::pack(f[0], f[1]), T16<DT>::pack(f[2], f[3]), T16<DT>::pack(f[4], f[5]), T16<DT>::pack(f[6], f[7])}, left,
-                  ((uintptr_t)y & 15) == 0);
+        store8_16(y, uint4v{T16<DT>::pack(f[0], f[1]), T16<DT>::pack(f[2], f[3]), T16<DT>::pack(f[4], f[5]), T16<DT>::pack(f[6], f[7])}, left);
     }
 }
 
@@ -173,7 +171,6 @@ int launch_mx_rows(const MxGemm& g, const void* x, long ldx, hipStream_t st) {
     r.g = g;
     r.x = (const uint16_t*)x;
     r.ldx = ldx;
-    r.xwide = (g.M == 1 || ldx % 8 == 0) && (uintptr_t)x % 16 == 0;
     return g.dtype == MQ_F16 ? choose_mx_rows<MQ_F16>(r, st) : choose_mx_rows<MQ_BF16>(r, st);
 }
 

@@ -1,25 +1,46 @@
 // Layer norm: forward (16-bit output, or straight into microscaled 4-bit floats) and backward.
 //
-// A row is held in registers by 64 lanes (up to 2048 columns) or by a workgroup (up to 16384), eight consecutive values per lane and step, so that
-// it is read once: mean, then the sum of squared deviations from it, then the output.  All sums are taken in fp32.
+// A row is held in registers by 8, 16, 32 or 64 lanes, so that each has three to five vectors of eight consecutive values (320, 640 and 1280 columns fill
+// them without a rest), or by a workgroup (up to 16384 columns), and is read once: mean, then the sum of squared deviations from it, then the output.
+// All sums are taken in fp32.  Bound by memory.  us: forward 16384 x 640 10.4 (4.0 TB/s), 2964 x 1280 5.5, 32768 x 2048 41 (6.5 TB/s), into MXFP4 9.4, 5.6
+// and 38; backward 20 (4.2 TB/s with a residual), 11.5 and 82.  (One row per wave of 64 lanes whatever its length: forward 13.8, 6.9, 50.)
+#include <type_traits>
+
 #include "mx_common.h"
 
 namespace mq {
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float swap_sum16(float v) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float((uint32_t)p[0]) + __uint_as_float((uint32_t)p[1]);
+}
+__device__ __forceinline__ float swap_sum32(float v) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float((uint32_t)p[0]) + __uint_as_float((uint32_t)p[1]);
+}
+// Sum over aligned runs of LANES lanes (8 to 64), the same bits in each of them.
+template <int LANES>
+__device__ __forceinline__ float lane_sum(float v) {
+    v += dpp<0xB1>(v);   // lanes 1,0,3,2 of four
+    v += dpp<0x4E>(v);   // lanes 2,3,0,1
+    v += dpp<0x141>(v);  // mirror of eight
+    if constexpr (LANES >= 16) v += dpp<0x140>(v);  // mirror of sixteen
+    if constexpr (LANES >= 32) v = swap_sum16(v);
+    if constexpr (LANES >= 64) v = swap_sum32(v);
     return v;
 }
 
-// Sum over the lanes that share a row.  `slot` (LDS, a workgroup's four waves): unused for 64 lanes.
+// Sum over the lanes that share a row.  `slot` (LDS, one per wave): where that is a workgroup.
 template <int LPR>
 __device__ __forceinline__ float row_sum(float v, float* slot) {
-    v = wave_sum(v);
+    v = lane_sum<LPR < 64 ? LPR : 64>(v);
     if constexpr (LPR == 256) {
-        const int wv = threadIdx.x >> 6;
         __syncthreads();
-        if ((threadIdx.x & 63) == 0) slot[wv] = v;
+        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
         __syncthreads();
         v = (slot[0] + slot[1]) + (slot[2] + slot[3]);
     }
@@ -43,7 +64,7 @@ __device__ __forceinline__ void load_params(const void* p, int dtype, int k, int
         }
     } else {
         const uint16_t* h = (const uint16_t*)p + k;
-        const uint4v v = load8_16(h, n, ((uintptr_t)h & 15) == 0);
+        const uint4v v = load8_16(h, n);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint16_t b = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
@@ -61,23 +82,81 @@ template <int DT>
 __device__ __forceinline__ uint4v narrow8(const float* f) {
     return uint4v{T16<DT>::pack(f[0], f[1]), T16<DT>::pack(f[2], f[3]), T16<DT>::pack(f[4], f[5]), T16<DT>::pack(f[6], f[7])};
 }
-__device__ __forceinline__ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-template <int DT, int LPR, int VPT, bool MX>
+// A workgroup's rows of a 16-bit matrix.  WIDE (rows on 16-byte boundaries, whole vectors of eight): through a buffer resource, so that what does not exist
+// reads as zero and is not written without a branch, and all loads of a row are under way at once.  Otherwise value by value where need be.
+template <bool WIDE>
+struct Rows {
+    const uint16_t* p;
+    long ld;
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ __forceinline__ Rows(const uint16_t* base, long ld_, long row0, long rows, int C) : p(base + row0 * ld_), ld(ld_) {
+        const long bytes = rows > 0 && base ? ((rows - 1) * ld + C) * 2 : 0;
+        if constexpr (WIDE) rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+    }
+    // Eight values from column k of row r (of the workgroup's), of which n exist.
+    __device__ __forceinline__ uint4v load(int r, int k, int n) const {
+        if constexpr (WIDE) return __builtin_amdgcn_raw_buffer_load_b128(rsrc, n > 0 ? (int)(r * ld + k) * 2 : -16, 0, 0);
+        const uint16_t* q = p + r * ld + k;
+        return n > 0 ? load8_16(q, n) : uint4v{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void store(int r, int k, int n, uint4v v) const {
+        if constexpr (WIDE) return __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, n > 0 ? (int)(r * ld + k) * 2 : -16, 0, 0);
+        uint16_t* q = (uint16_t*)p + r * ld + k;
+        if (n > 0) store8_16(q, v, n);
+    }
+};
+
+// Parameters of VPT vectors of columns, loaded ahead of their use.
+template <int VPT, bool WIDE, bool F32>
+struct Params {
+    uint4v raw[WIDE ? VPT : 1][F32 ? 2 : 1];
+    const void* p;
+    int dtype;
+    __device__ __forceinline__ Params(const void* p_, int dtype_, int C, int LPR, int li) : p(p_), dtype(dtype_) {
+        if constexpr (WIDE) {
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, C * (F32 ? 4 : 2), 0x00020000);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int q = 0; q < (F32 ? 2 : 1); ++q)
+                    raw[i][q] = __builtin_amdgcn_raw_buffer_load_b128(r, (i * LPR + li) * (F32 ? 32 : 16) + q * 16, 0, 0);
+        }
+    }
+    template <int DT>
+    __device__ __forceinline__ void get(int i, int k, int n, float fill, float* out) const {
+        if constexpr (!WIDE) {
+            if (n > 0) load_params(p, dtype, k, n, fill, out);
+        } else if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) out[e] = __uint_as_float(raw[i][e >> 2][e & 3]);
+        } else {
+            widen8<DT>(raw[i][0], out);
+        }
+    }
+};
+
+template <int DT, int LPR, int VPT, bool MX, bool WIDE, bool F32>
 __global__ __launch_bounds__(256) void layer_norm_kernel(const NormArgs g, const int kc, const int kq) {
+    constexpr int RPW = 256 / LPR;
     __shared__ float slot[4];
-    const int li = threadIdx.x % LPR;
-    const long row = (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const int li = threadIdx.x % LPR, ri = threadIdx.x / LPR;
+    const long row0 = (long)blockIdx.x * RPW, row = row0 + ri;
     const bool real = row < g.M;  // (MX: rows of padding up to a multiple of 32 are written as zeros)
-    if (!MX && LPR == 64 && !real) return;
-    const uint16_t* x = g.x + row * g.ldx;
-    const bool wide = aligned16(x);
+    const long rows = g.M - row0 < RPW ? g.M - row0 : RPW;
+    const Rows<WIDE> x(g.x, g.ldx, row0, rows, g.C);
+    uint4v raw[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        const int k = (i * LPR + li) * 8;
+        raw[i] = x.load(ri, k, real ? g.C - k : 0);
+    }
+    const Params<VPT, WIDE, F32> weight(g.weight, g.param_dtype, g.C, LPR, li), bias(g.bias, g.param_dtype, g.C, LPR, li);
     float v[VPT][8];
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        const int k = (i * LPR + li) * 8, n = real ? g.C - k : 0;
-        widen8<DT>(n > 0 ? load8_16(x + k, n, wide) : uint4v{0, 0, 0, 0}, v[i]);
+        widen8<DT>(raw[i], v[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += v[i][e];
     }
@@ -98,21 +177,22 @@ __global__ __launch_bounds__(256) void layer_norm_kernel(const NormArgs g, const
         if (g.mean) g.mean[row] = mean;
         if (g.rstd) g.rstd[row] = rstd;
     }
-    uint16_t* y = MX ? nullptr : g.y + row * g.ldy;
-    const bool ywide = aligned16(y);
+    const long grp = row >> 5;
+    auto codes_of = [&](int c, int kb) { return (uint8_t*)g.mx + (grp * kc + c) * 1024 + (kb * 32 + (row & 31)) * 16; };
+    auto scale_of = [&](int c, int kb) {
+        return (uint8_t*)g.mx + ((long)g.M + 31) / 32 * kc * 1024 + (grp * kq + (c >> 2)) * 256 + (kb * 32 + (row & 31)) * 4 + (c & 3);
+    };
+    const Rows<WIDE && !MX> y(g.y, g.ldy, row0, rows, g.C);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         const int k = (i * LPR + li) * 8, n = g.C - k;
-        if (!MX && n <= 0) break;
         float w[8], b[8], o[8];
-        if (n > 0) {
-            load_params(g.weight, g.param_dtype, k, n, 1.0f, w);
-            load_params(g.bias, g.param_dtype, k, n, 0.0f, b);
-        }
+        weight.template get<DT>(i, k, n, 1.0f, w);
+        bias.template get<DT>(i, k, n, 0.0f, b);
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = n > 0 ? v[i][e] * rstd * w[e] + b[e] : 0.0f;
         if constexpr (!MX) {
-            if (real) store8_16(y + k, narrow8<DT>(o), n, ywide);
+            y.store(ri, k, real ? n : 0, narrow8<DT>(o));
         } else {
             uint32_t top = 0;
 #pragma unroll
@@ -126,36 +206,66 @@ __global__ __launch_bounds__(256) void layer_norm_kernel(const NormArgs g, const
             uint32_t codes = mx_codes_f32(o, mx_scale_operand(sb));
             if (!in || sb == 255u) codes = 0;
             const int c = k >> 6, kb = (k >> 5) & 1, part = li & 3;
-            const long grp = row >> 5;
-            const int L = kb * 32 + (int)(row & 31);
-            uint8_t* scales = (uint8_t*)g.mx + ((long)g.M + 31) / 32 * kc * 1024;
-            if (c < kc) *(uint32_t*)((uint8_t*)g.mx + (grp * kc + c) * 1024 + L * 16 + part * 4) = codes;
-            if (part == 0 && c < kq * 4) scales[(grp * kq + (c >> 2)) * 256 + L * 4 + (c & 3)] = (uint8_t)sb;
+            if (c < kc) *(uint32_t*)(codes_of(c, kb) + part * 4) = codes;
+            if (part == 0 && c < kq * 4) *scale_of(c, kb) = (uint8_t)sb;
+        }
+    }
+    if constexpr (MX) {  // padding that no lane came by
+        for (int b = LPR * VPT / 4 + li; b < kq * 8; b += LPR) {
+            if (b >> 1 < kc) *(uint4v*)codes_of(b >> 1, b & 1) = uint4v{0, 0, 0, 0};
+            *scale_of(b >> 1, b & 1) = 0;
         }
     }
 }
 
+// Calls go(lanes per row, vectors per lane) with the form for `vecs` vectors of eight columns.
+template <class F>
+static void norm_form(int vecs, F go) {
+    auto lanes = [&](auto lpr) {
+        constexpr int L = decltype(lpr)::value;
+        if (vecs <= 3 * L)
+            go(lpr, std::integral_constant<int, 3>{});
+        else if (vecs <= 4 * L)
+            go(lpr, std::integral_constant<int, 4>{});
+        else
+            go(lpr, std::integral_constant<int, 5>{});
+    };
+    if (vecs <= 40)
+        lanes(std::integral_constant<int, 8>{});
+    else if (vecs <= 80)
+        lanes(std::integral_constant<int, 16>{});
+    else if (vecs <= 160)
+        lanes(std::integral_constant<int, 32>{});
+    else if (vecs <= 320)
+        lanes(std::integral_constant<int, 64>{});
+    else if (vecs <= 512)
+        go(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
+    else if (vecs <= 1280)
+        lanes(std::integral_constant<int, 256>{});
+    else
+        go(std::integral_constant<int, 256>{}, std::integral_constant<int, 8>{});
+}
+
+// Whole vectors of eight on 16-byte boundaries, rows of a workgroup within 32-bit offsets; parameters present, fp32 or of the rows' type.
+static bool wide_matrix(const void* p, long ld, int M, int C) { return C % 8 == 0 && (M == 1 || ld % 8 == 0) && (uintptr_t)p % 16 == 0 && ld < (1 << 24); }
+static bool wide_params(const void* p, const NormArgs& a) { return p && (uintptr_t)p % 16 == 0 && (a.param_dtype == MQ_F32 || a.param_dtype == a.dtype); }
+
 template <int DT, bool MX>
 static int forward(const NormArgs& a, hipStream_t st) {
     const int kc = (a.C + 63) / 64, kq = (kc + 3) / 4;
-    // columns that the lanes have to cover: all that exist, or all of the scales' padding
-    const int cols = MX ? kq * 256 : a.C;
     const long rows = MX ? ((long)a.M + 31) / 32 * 32 : a.M;
-    auto go = [&](auto kernel, int rows_per_wg) { kernel<<<(unsigned)((rows + rows_per_wg - 1) / rows_per_wg), 256, 0, st>>>(a, kc, kq); };
-    if (cols <= 512)
-        go(layer_norm_kernel<DT, 64, 1, MX>, 4);
-    else if (cols <= 1024)
-        go(layer_norm_kernel<DT, 64, 2, MX>, 4);
-    else if (cols <= 1536)
-        go(layer_norm_kernel<DT, 64, 3, MX>, 4);
-    else if (cols <= 2048)
-        go(layer_norm_kernel<DT, 64, 4, MX>, 4);
-    else if (cols <= 4096)
-        go(layer_norm_kernel<DT, 256, 2, MX>, 1);
-    else if (cols <= 8192)
-        go(layer_norm_kernel<DT, 256, 4, MX>, 1);
-    else
-        go(layer_norm_kernel<DT, 256, 8, MX>, 1);
+    norm_form((a.C + 7) / 8, [&](auto lpr, auto vpt) {
+        constexpr int L = decltype(lpr)::value, RPW = 256 / L;
+        constexpr int V = decltype(vpt)::value;
+        const unsigned grid = (unsigned)((rows + RPW - 1) / RPW);
+        const bool wide = wide_matrix(a.x, a.ldx, a.M, a.C) && (MX || wide_matrix(a.y, a.ldy, a.M, a.C)) && wide_params(a.weight, a) && wide_params(a.bias, a);
+        if (!wide)
+            layer_norm_kernel<DT, L, V, MX, false, false><<<grid, 256, 0, st>>>(a, kc, kq);
+        else if (a.param_dtype == MQ_F32)
+            layer_norm_kernel<DT, L, V, MX, true, true><<<grid, 256, 0, st>>>(a, kc, kq);
+        else
+            layer_norm_kernel<DT, L, V, MX, true, false><<<grid, 256, 0, st>>>(a, kc, kq);
+    });
     MQ_HIP_CHECK_LAUNCH();
     return MQ_OK;
 }
@@ -164,13 +274,12 @@ int launch_layer_norm_mx(const NormArgs& a, hipStream_t st) { return a.dtype == 
 
 // Backward.  With xhat = (x - mean) rstd and g = dy weight:  dx = rstd (g - mean(g) - xhat mean(g xhat)) (+ residual);
 // dweight = sum over rows of dy xhat, dbias = sum over rows of dy.  A workgroup walks its share of the rows, each lane adding up the columns that it
-// holds anyway; the sums of its waves are joined in LDS in wave order and written to the workspace, and a second kernel adds the workgroups' in order:
-// the result does not depend on timing.
-template <int DT, int LPR, int VPT>
+// holds anyway; lanes and waves with the same columns are joined in a fixed order and written to the workspace, and a second kernel adds the
+// workgroups' in order: the result does not depend on timing.
+template <int DT, int LPR, int VPT, bool WIDE, bool F32>
 __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormArgs g) {
-    constexpr int RPW = 256 / LPR;
-    extern __shared__ float sums[];  // [2][C] where several rows share a workgroup
-    __shared__ float slot[4];
+    constexpr int RPW = 256 / LPR, COLS = LPR * VPT * 8;
+    __shared__ __attribute__((aligned(16))) float sums[LPR < 256 ? RPW * COLS : 4];  // LPR == 256: for row_sum
     const int li = threadIdx.x % LPR, ri = threadIdx.x / LPR;
     const float inv = 1.0f / (float)g.C;
     float aw[VPT][8], ab[VPT][8];
@@ -178,133 +287,174 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormArgs g) 
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) aw[i][e] = ab[i][e] = 0.0f;
-    for (long row0 = (long)blockIdx.x * RPW; row0 < g.M; row0 += (long)gridDim.x * RPW) {
-        const long row = row0 + ri;
-        const bool real = row < g.M;
-        const float mean = real ? g.mean[row] : 0.0f, rstd = real ? g.rstd[row] : 0.0f;
-        const uint16_t *x = g.x + row * g.ldx, *dy = g.dy + row * g.lddy;
-        const bool xw = aligned16(x), dw = aligned16(dy);
+    const Params<VPT, WIDE, F32> weight(g.weight, g.param_dtype, g.C, LPR, li);
+    // The rows after these are on their way while these are worked on.
+    uint4v rx[VPT], rd[VPT], rr[VPT];
+    float mean = 0.0f, rstd = 0.0f;
+    auto rows_at = [&](long row0) { return g.M - row0 < RPW ? g.M - row0 : RPW; };
+    auto load = [&](long row0) {
+        const long rows = rows_at(row0);
+        const Rows<WIDE> x(g.x, g.ldx, row0, rows, g.C), dy(g.dy, g.lddy, row0, rows, g.C);
+        const bool real = ri < rows;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int k = (i * LPR + li) * 8, n = real ? g.C - k : 0;
+            rx[i] = x.load(ri, k, n);
+            rd[i] = dy.load(ri, k, n);
+        }
+        mean = real ? g.mean[row0 + ri] : 0.0f;
+        rstd = real ? g.rstd[row0 + ri] : 0.0f;
+    };
+    auto load_residual = [&](long row0) {
+        if (!g.res) return;
+        const long rows = rows_at(row0);
+        const Rows<WIDE> res(g.res, g.ldr, row0, rows, g.C);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int k = (i * LPR + li) * 8;
+            rr[i] = res.load(ri, k, ri < rows ? g.C - k : 0);
+        }
+    };
+    const long stride = (long)gridDim.x * RPW;
+    long row0 = (long)blockIdx.x * RPW;
+    if (WIDE) load(row0), load_residual(row0);
+    for (; row0 < g.M; row0 += stride) {
+        if (!WIDE) load(row0), load_residual(row0);  // (pieces of vectors take too many registers to have two rows of)
+        const float m = mean, r = rstd;
         float xh[VPT][8], gr[VPT][8];
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int k = (i * LPR + li) * 8, n = real ? g.C - k : 0;
+            const int k = (i * LPR + li) * 8, n = g.C - k;
             float d[8], w[8];
-            widen8<DT>(n > 0 ? load8_16(x + k, n, xw) : uint4v{0, 0, 0, 0}, xh[i]);
-            widen8<DT>(n > 0 ? load8_16(dy + k, n, dw) : uint4v{0, 0, 0, 0}, d);
-            if (n > 0) load_params(g.weight, g.param_dtype, k, n, 1.0f, w);
+            widen8<DT>(rx[i], xh[i]);
+            widen8<DT>(rd[i], d);  // zero where there is no value
+            weight.template get<DT>(i, k, n, 1.0f, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                xh[i][e] = e < n ? (xh[i][e] - mean) * rstd : 0.0f;
-                gr[i][e] = e < n ? d[e] * w[e] : 0.0f;
-                if (e < n) {
-                    aw[i][e] += d[e] * xh[i][e];
-                    ab[i][e] += d[e];
-                }
+                xh[i][e] = (xh[i][e] - m) * r;
+                gr[i][e] = WIDE || e < n ? d[e] * w[e] : 0.0f;
+                aw[i][e] += d[e] * xh[i][e];
+                ab[i][e] += d[e];
                 s1 += gr[i][e];
                 s2 += gr[i][e] * xh[i][e];
             }
         }
-        s1 = row_sum<LPR>(s1, slot) * inv;
-        s2 = row_sum<LPR>(s2, slot) * inv;
-        if (!real) continue;
-        uint16_t* dx = g.dx + row * g.lddx;
-        const bool ow = aligned16(dx);
-        const uint16_t* res = g.res ? g.res + row * g.ldr : nullptr;
-        const bool rw = aligned16(res);
+        if (WIDE && row0 + stride < g.M) load(row0 + stride);
+        s1 = row_sum<LPR>(s1, sums) * inv;
+        s2 = row_sum<LPR>(s2, sums) * inv;
+        const long rows = rows_at(row0);
+        const Rows<WIDE> dx(g.dx, g.lddx, row0, rows, g.C);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int k = (i * LPR + li) * 8, n = g.C - k;
-            if (n <= 0) break;
-            float o[8], r[8];
-            if (res) widen8<DT>(load8_16(res + k, n, rw), r);
+            float o[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = (gr[i][e] - s1 - xh[i][e] * s2) * rstd + (res ? r[e] : 0.0f);
-            store8_16(dx + k, narrow8<DT>(o), n, ow);
+            for (int e = 0; e < 8; ++e) o[e] = (gr[i][e] - s1 - xh[i][e] * s2) * r;
+            if (g.res) {
+                float a[8];
+                widen8<DT>(rr[i], a);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] += a[e];
+            }
+            dx.store(ri, k, ri < rows ? n : 0, narrow8<DT>(o));
         }
+        if (WIDE && row0 + stride < g.M) load_residual(row0 + stride);
     }
     float* out = g.partial + (long)blockIdx.x * 2 * g.C;
-    if constexpr (LPR == 64) {
-        for (int w = 0; w < RPW; ++w) {
-            if (ri == w) {
 #pragma unroll
-                for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int k = (i * LPR + li) * 8 + e;
-                        if (k < g.C) {
-                            sums[k] = (w ? sums[k] : 0.0f) + aw[i][e];
-                            sums[g.C + k] = (w ? sums[g.C + k] : 0.0f) + ab[i][e];
-                        }
-                    }
-            }
+    for (int which = 0; which < 2; ++which) {  // one of the two sums after the other: the rows' sums of a column lie below one another
+        const float(&acc)[VPT][8] = which ? ab : aw;
+        if constexpr (LPR < 256) {
             __syncthreads();
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    *(float4v*)(sums + ri * COLS + (i * LPR + li) * 8 + q * 4) = float4v{acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
+            __syncthreads();
+            for (int k = threadIdx.x; k < g.C; k += 256) {
+                float v = sums[k];
+#pragma unroll
+                for (int j = 1; j < RPW; ++j) v += sums[j * COLS + k];
+                out[which * g.C + k] = v;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int k = (i * LPR + li) * 8 + e;
+                    if (k < g.C) out[which * g.C + k] = acc[i][e];
+                }
         }
-        for (int k = threadIdx.x; k < 2 * g.C; k += 256) out[k] = sums[k];
+    }
+}
+
+// Adds the workgroups' sums, column by column, in order: 32 columns per workgroup, and 32 runs of parts side by side.
+__global__ __launch_bounds__(256) void layer_norm_join_kernel(const float* partial, int parts, int C, float* dweight, float* dbias) {
+    __shared__ float run[32][33];
+    const int col = threadIdx.x & 7, r = threadIdx.x >> 3;
+    const int k = blockIdx.x * 32 + col * 4;  // of 2 C
+    const int per = (parts + 31) / 32, p0 = r * per, p1 = p0 + per < parts ? p0 + per : parts;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (k + 4 <= 2 * C && C % 2 == 0) {
+#pragma unroll 8
+        for (int p = p0; p < p1; ++p) {
+            const float4v v = *(const float4v*)(partial + (long)p * 2 * C + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += v[e];
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i)
+        for (int e = 0; e < 4; ++e)
+            if (k + e < 2 * C)
+                for (int p = p0; p < p1; ++p) s[e] += partial[(long)p * 2 * C + k + e];
+    }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int k = (i * LPR + li) * 8 + e;
-                if (k < g.C) {
-                    out[k] = aw[i][e];
-                    out[g.C + k] = ab[i][e];
-                }
-            }
-    }
-}
-
-// Adds the workgroups' sums, column by column, in order: 16 runs of them per column side by side.
-__global__ __launch_bounds__(256) void layer_norm_join_kernel(const float* partial, int parts, int C, float* dweight, float* dbias) {
-    __shared__ float run[16][16];
-    const int col = threadIdx.x & 15, r = threadIdx.x >> 4;
-    const int k = blockIdx.x * 16 + col;  // of 2 C
-    const int per = (parts + 15) / 16, p0 = r * per, p1 = p0 + per < parts ? p0 + per : parts;
-    float s = 0.0f;
-    if (k < 2 * C)
-        for (int p = p0; p < p1; ++p) s += partial[(long)p * 2 * C + k];
-    run[r][col] = s;
+    for (int e = 0; e < 4; ++e) run[r][col * 4 + e] = s[e];
     __syncthreads();
-    if (r == 0 && k < 2 * C) {
-        s = run[0][col];
-        for (int i = 1; i < 16; ++i) s += run[i][col];
-        float* out = k < C ? dweight : dbias;
-        if (out) out[k < C ? k : k - C] = s;
+    const int j = blockIdx.x * 32 + threadIdx.x;
+    if (threadIdx.x < 32 && j < 2 * C) {
+        float t = run[0][threadIdx.x];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) t += run[i][threadIdx.x];
+        float* out = j < C ? dweight : dbias;
+        if (out) out[j < C ? j : j - C] = t;
     }
 }
 
-static int grad_rows_per_wg(long C) { return C <= 2048 ? 4 : 1; }
+// Rows that a workgroup has in registers at a time, and the number of workgroups: one per compute unit (a wave's registers leave room for one, and the
+// sums of two would only be more to join; us, 256 / 512 workgroups: 16384 x 640 20.1 / 24.5, 2964 x 1280 11.5 / 15.4, 32768 x 2048 81.6 / 83.5).
+static int grad_rows_per_wg(long C) {
+    const long v = (C + 7) / 8;
+    return v <= 40 ? 32 : v <= 80 ? 16 : v <= 160 ? 8 : v <= 320 ? 4 : 1;
+}
 static long grad_workgroups(long M, long C) {
     const long n = (M + grad_rows_per_wg(C) - 1) / grad_rows_per_wg(C);
-    return n < 512 ? n : 512;
+    return n < 256 ? n : 256;
 }
 size_t layer_norm_grad_workspace_bytes(long M, long C) { return (size_t)grad_workgroups(M, C) * 2 * (size_t)C * 4; }
 
 template <int DT>
 static int backward(const NormArgs& a, hipStream_t st) {
     const long parts = grad_workgroups(a.M, a.C);
-    auto go = [&](auto kernel, size_t lds) { kernel<<<(unsigned)parts, 256, lds, st>>>(a); };
-    const size_t lds = (size_t)a.C * 8;
     if (parts > 0) {
-        if (a.C <= 512)
-            go(layer_norm_grad_kernel<DT, 64, 1>, lds);
-        else if (a.C <= 1024)
-            go(layer_norm_grad_kernel<DT, 64, 2>, lds);
-        else if (a.C <= 1536)
-            go(layer_norm_grad_kernel<DT, 64, 3>, lds);
-        else if (a.C <= 2048)
-            go(layer_norm_grad_kernel<DT, 64, 4>, lds);
-        else if (a.C <= 4096)
-            go(layer_norm_grad_kernel<DT, 256, 2>, 0);
-        else if (a.C <= 8192)
-            go(layer_norm_grad_kernel<DT, 256, 4>, 0);
-        else
-            go(layer_norm_grad_kernel<DT, 256, 8>, 0);
+        norm_form((a.C + 7) / 8, [&](auto lpr, auto vpt) {
+            constexpr int L = decltype(lpr)::value, V = decltype(vpt)::value;
+            const bool wide = wide_matrix(a.x, a.ldx, a.M, a.C) && wide_matrix(a.dy, a.lddy, a.M, a.C) && wide_matrix(a.dx, a.lddx, a.M, a.C) &&
+                              (!a.res || wide_matrix(a.res, a.ldr, a.M, a.C)) && wide_params(a.weight, a);
+            if (!wide)
+                layer_norm_grad_kernel<DT, L, V, false, false><<<(unsigned)parts, 256, 0, st>>>(a);
+            else if (a.param_dtype == MQ_F32)
+                layer_norm_grad_kernel<DT, L, V, true, true><<<(unsigned)parts, 256, 0, st>>>(a);
+            else
+                layer_norm_grad_kernel<DT, L, V, true, false><<<(unsigned)parts, 256, 0, st>>>(a);
+        });
         MQ_HIP_CHECK_LAUNCH();
     }
     if (a.dweight || a.dbias) {
-        layer_norm_join_kernel<<<(2 * a.C + 15) / 16, 256, 0, st>>>(a.partial, (int)parts, a.C, a.dweight, a.dbias);
+        layer_norm_join_kernel<<<(2 * a.C + 31) / 32, 256, 0, st>>>(a.partial, (int)parts, a.C, a.dweight, a.dbias);
         MQ_HIP_CHECK_LAUNCH();
     }
     return MQ_OK;
