@@ -165,6 +165,25 @@ def test_linear(mq, M, K, N, dtype):
     check_linear(mq, x, w, None, rand((M, N), dtype, 10), packed=True)
 
 
+@pytest.mark.parametrize("M,K,N", ((8200, 704, 4104), (33000, 320, 1032), (2400, 640, 1944), (1190, 992, 4200), (6000, 1280, 1600)))
+def test_linear_tiles(mq, M, K, N):
+    """Several tiles for a workgroup, large ones and ones of another shape, last ones that are cut off on both sides; every element, with and without a
+    residual, in place too."""
+    x, w, b, r = rand((M, K), F16, 11), rand((N, K), F16, 12, 0.02), rand((N,), F16, 13, 0.1), rand((M, N), F16, 14)
+    wq, xq = mq.mx_quantize_weights(w), mq.mx_quantize(x)
+    xv, wv = mq.mx_dequantize(xq, BF16).double(), mq.mx_dequantize(wq, BF16).double()  # (exact: two significant bits)
+    want, mag = xv @ wv.T + b.double(), xv.abs() @ wv.abs().T + b.double().abs()
+    for res in (None, r):
+        if res is not None:
+            want, mag = want + res.double(), mag + res.double().abs()
+        y = mq.mx_linear(xq, wq, b, residual=res, dtype=F16)
+        acc = (K + 4) * 2 * U * mag
+        bound = acc + torch.finfo(F16).eps / 2 * (want.abs() + acc) + 2.0 ** -25
+        assert int(((y.double() - want).abs() > bound).sum()) == 0
+    o = r.clone()
+    assert torch.equal(mq.mx_linear(xq, wq, b, residual=o, dtype=F16, out=o), y)
+
+
 @pytest.mark.parametrize("M", (1, 5, 40, 200))
 def test_linear_views(mq, M):
     """Strides and alignments of every operand; the residual as the output itself; the output over the activations."""
