@@ -101,7 +101,7 @@ struct Rows {
         return n > 0 ? load8_16(q, n) : uint4v{0, 0, 0, 0};
     }
     __device__ __forceinline__ void store(int r, int k, int n, uint4v v) const {
-        if constexpr (WIDE) return __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, n > 0 ? (int)(r * ld + k) * 2 : -16, 0, 0);
+        if constexpr (WIDE) return __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, n > 0 ? (int)(r * ld + k) * 2 : -16, 0, WRITE_THROUGH);
         uint16_t* q = (uint16_t*)p + r * ld + k;
         if (n > 0) store8_16(q, v, n);
     }
