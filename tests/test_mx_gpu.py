@@ -512,3 +512,17 @@ def test_graph_replays_and_side_stream(mq):
         torch.cuda.synchronize()
         for a, c in zip(captured, step(mq, x, gain, shift, wq, bias, dy, res)):
             assert torch.equal(a, c)
+
+
+# ------------------------------------------------------------------------------------------------------------ together
+
+def test_example_tunes_norms(mq):
+    """The operators as a training loop uses them: the error against the 16-bit blocks falls."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "tune_norms.py")
+    spec = importlib.util.spec_from_file_location("tune_norms", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    losses = m.tune(rows=500, width=160, hidden=608, blocks=2, steps=40, say=lambda *a, **k: None)
+    assert all(np.isfinite(losses)) and np.mean(losses[-5:]) < np.mean(losses[:5])
