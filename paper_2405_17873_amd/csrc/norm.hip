@@ -2,8 +2,9 @@
 //
 // A row is held in registers by 8, 16, 32 or 64 lanes, so that each has three to five vectors of eight consecutive values (320, 640 and 1280 columns fill
 // them without a rest), or by a workgroup (up to 16384 columns), and is read once: mean, then the sum of squared deviations from it, then the output.
-// All sums are taken in fp32.  Bound by memory.  us: forward 16384 x 640 10.4 (4.0 TB/s), 2964 x 1280 5.5, 32768 x 2048 41 (6.5 TB/s), into MXFP4 9.4, 5.6
-// and 38; backward 20 (4.2 TB/s with a residual), 11.5 and 82.  (One row per wave of 64 lanes whatever its length: forward 13.8, 6.9, 50.)
+// All sums are taken in fp32.  Bound by memory.  us: forward 16384 x 640 8.0 (5.2 TB/s), 2964 x 1280 4.8, 32768 x 2048 39 (6.8 TB/s), into MXFP4 9.5, 5.6
+// and 39; backward 19.5 (4.3 TB/s with a residual), 10.9 and 79.  (One row per wave of 64 lanes whatever its length, before stores went through: forward 13.8,
+// 6.9, 50, when these took 10.4, 5.5, 41.)
 #include <type_traits>
 
 #include "mx_common.h"
