@@ -28,10 +28,10 @@ __device__ __forceinline__ void mx_swap16(uint4v* v) {
         v[1][i] = (uint32_t)p[1];
     }
 }
-// Adds bias and residual r[2] (in the order of the output, or null) to a block's sums and brings them into the order of the output: two vectors of eight
+// Adds a residual r[2] (in the order of the output, or null) to a block's sums and brings them into the order of the output: two vectors of eight
 // columns, of rows lane & 15 and 16 further on, columns 16 q + 8 h (q, h: bits 4 and 5 of the lane).
 template <int DT>
-__device__ __forceinline__ void mx_finish_block(const float16v& acc, const uint2v* bias, const uint4v* r, uint4v* v) {
+__device__ __forceinline__ void mx_finish_block(const float16v& acc, const uint4v* r, uint4v* v) {
     if (r) {
         v[0] = r[0], v[1] = r[1];
         mx_swap16(v);
@@ -40,7 +40,7 @@ __device__ __forceinline__ void mx_finish_block(const float16v& acc, const uint2
     for (int t = 0; t < 2; ++t) {
         float f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = acc[8 * t + i] + T16<DT>::up((uint16_t)(bias[2 * t + (i >> 2)][(i >> 1) & 1] >> (16 * (i & 1))));
+        for (int i = 0; i < 8; ++i) f[i] = acc[8 * t + i];
         if (r) {
             const auto p = __builtin_amdgcn_permlane32_swap(v[t][0], v[t][2], false, false), q = __builtin_amdgcn_permlane32_swap(v[t][1], v[t][3], false, false);
             const uint32_t o[4] = {(uint32_t)p[0], (uint32_t)q[0], (uint32_t)p[1], (uint32_t)q[1]};
@@ -240,13 +240,32 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void mx_gemm_kernel(const MxGemm g
 
     int behind = 0;  // steps to come whose slots were asked for ahead of stores
     for (; at < end; at += every, behind = EPI != MX_ODD ? S - 2 : 0) {
+        // The sums start from the bias, which costs their end 16 additions a block less.
+        int tr, tc;
+        mx_tile(at, tiles, tr, tc);
+        const long m0 = (long)tr * (P::GA * 32) + wm * TM * 32;
+        const int n0 = tc * (P::GB * 32) + wn * TN * 32, q = (lane >> 4) & 1, c0 = n0 + 16 * q + 8 * h;
 #pragma unroll
         for (int n = 0; n < TN; ++n)
 #pragma unroll
-            for (int m = 0; m < TM; ++m)
+            for (int t = 0; t < 4; ++t) {
+                uint2v bias = {0, 0};
+                if constexpr (EPI != MX_ODD) {
+                    bias = *(const lds_uint2v*)(uintptr_t)(lds0 + slot + P::BIAS + ((wn * TN + n) * 32 + 8 * t + 4 * h) * 2);
+                } else if (g.bias) {
+                    const int c = n0 + n * 32 + 8 * t + 4 * h;
+                    if (c + 4 <= g.N) bias = *(const uint2v_any*)(g.bias + c);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.0f;
-        uint2v bias[TN][4];
+                    for (int i = 0; i < 4; ++i)
+                        if (c + 4 > g.N && c + i < g.N) bias[i >> 1] |= (uint32_t)g.bias[c + i] << (16 * (i & 1));
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float f = T16<DT>::up((uint16_t)(bias[i >> 1] >> (16 * (i & 1))));
+#pragma unroll
+                    for (int m = 0; m < TM; ++m) acc[m][n][4 * t + i] = f;
+                }
+            }
         after = source(at + every);
         auto do_step = [&](int step) {
             Scales s;
@@ -272,18 +291,9 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void mx_gemm_kernel(const MxGemm g
                     read_scale(next, slot, j - READS);
             });
         };
-        for (int step = 0; step < steps - 1; ++step) do_step(step);  // (one block of code: MFMAs sink past the ends of blocks)
-        if constexpr (EPI != MX_ODD) {  // every step's slot has the bias; behind the last wait it may be overwritten
-#pragma unroll
-            for (int n = 0; n < TN; ++n)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) bias[n][t] = *(const lds_uint2v*)(uintptr_t)(lds0 + slot + P::BIAS + ((wn * TN + n) * 32 + 8 * t + 4 * h) * 2);
-        }
-        do_step(steps - 1);
-        int tr, tc;
-        mx_tile(at, tiles, tr, tc);
-        const long m0 = (long)tr * (P::GA * 32) + wm * TM * 32;
-        const int n0 = tc * (P::GB * 32) + wn * TN * 32, q = (lane >> 4) & 1, c0 = n0 + 16 * q + 8 * h;
+        int step = 0;
+        do do_step(step);  // (one block of code: MFMAs sink past the ends of blocks)
+        while (++step < steps);
         if constexpr (EPI != MX_ODD) {
             // Stores of a fixed number, whatever exists (what does not is dropped): the waits count them.
             const long rows = g.M - m0;
@@ -307,7 +317,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void mx_gemm_kernel(const MxGemm g
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) {
                 uint4v v[2];
-                mx_finish_block<DT>(acc[i / TN][i % TN], bias[i % TN], EPI == MX_RES ? r[EPI == MX_RES ? i : 0] : nullptr, v);
+                mx_finish_block<DT>(acc[i / TN][i % TN], EPI == MX_RES ? r[EPI == MX_RES ? i : 0] : nullptr, v);
                 if (i + AHEAD < BLOCKS) residual(i + AHEAD);  // (before the stores: waiting for it is not waiting for them)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) __builtin_amdgcn_raw_buffer_store_b128(v[t], ry, offset(g.ldy, i / TN, i % TN, t), 0, POLICY);
@@ -315,15 +325,6 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void mx_gemm_kernel(const MxGemm g
         } else {
 #pragma unroll
             for (int n = 0; n < TN; ++n) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int c = n0 + n * 32 + 8 * t + 4 * h;
-                    bias[n][t] = uint2v{0, 0};
-                    if (g.bias && c + 4 <= g.N) bias[n][t] = *(const uint2v_any*)(g.bias + c);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (g.bias && c + 4 > g.N && c + i < g.N) bias[n][t][i >> 1] |= (uint32_t)g.bias[c + i] << (16 * (i & 1));
-                }
                 const int c = c0 + n * 32, left = g.N - c;
 #pragma unroll
                 for (int m = 0; m < TM; ++m) {
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void mx_gemm_kernel(const MxGemm g
                         for (int t = 0; t < 2; ++t)
                             if (row + 16 * t < g.M && left > 0) r[t] = load8_16(g.res + (row + 16 * t) * g.ldr + c, left);
                     }
-                    mx_finish_block<DT>(acc[m][n], bias[n], r, v);
+                    mx_finish_block<DT>(acc[m][n], r, v);
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
                         if (row + 16 * t < g.M && left > 0) store8_16(g.y + (row + 16 * t) * g.ldy + c, v[t], left);
