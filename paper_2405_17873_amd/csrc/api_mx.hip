@@ -6,7 +6,6 @@
 namespace mq {
 
 static inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-static inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 static inline bool type_ok(int dtype) { return dtype == MQ_F16 || dtype == MQ_BF16; }
 
 // A matrix of 16-bit values with `cols` columns: rows may lie apart, and need not start on any boundary but their own type's.

@@ -141,6 +141,8 @@ __device__ __forceinline__ void store8_16(uint16_t* p, uint4v v, int n) {
     }
 }
 
+inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
 // ---- launchers (arguments are checked by the entry points) ----
 struct MxGemm {
     MxView a, w;  // activations [M,K], weights [N,K]

@@ -380,6 +380,20 @@ __global__ __launch_bounds__(256) void mx_grad_any_kernel(const MxGrad g) {
     }
 }
 
+// Rows of dY that do not start on 16-byte boundaries, or end inside a vector of eight, copied to rows that do neither; what is past their end is zero.
+// A wave takes 256 vectors of a row.
+__global__ __launch_bounds__(256) void mx_grad_align_kernel(const uint16_t* dy, long lddy, int M, int N, uint16_t* to, int ld) {
+    const long m = blockIdx.x * 4L + (threadIdx.x >> 6);
+    const int n0 = (int)blockIdx.y * 2048 + (threadIdx.x & 63) * 8;
+    if (m >= M) return;
+    uint4v v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = n0 + i * 512 < N ? load8_16(dy + m * lddy + n0 + i * 512, N - n0 - i * 512) : uint4v{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (n0 + i * 512 < N) *(uint4v*)(to + m * ld + n0 + i * 512) = v[i];
+}
+
 // The form for a problem: 32, 64 or 128 rows of a tile, and how the last round of tiles is cut, by what it is estimated to take: a launch, and for every
 // round of 256 workgroups a fixed part (filling the pipeline, joining the waves) and one per unit of a wave.  us, estimate (measured) for 32 / 64 / 128
 // rows: 308 x 2048 x 640 8.1 (7.5) / 9.9 (9.0) / 11.9 (11.7), 1000 x 992 x 1000 9.6 (9.1) / 11.9 (10.9) / 15 (14), 4096 x 1280 x 1280 43 (43) / 35 (35) /
@@ -411,9 +425,16 @@ static GradForm mx_grad_form(long M, long N, long K) {
     const int i = f[1].us < f[0].us ? 1 : 0;
     return f[2].us < f[i].us ? f[2] : f[i];
 }
-size_t mx_grad_workspace_bytes(long M, long N, long K) {
+static size_t mx_grad_partial_bytes(long M, long N, long K) {
     const GradForm f = mx_grad_form(M, N, K);
     return f.parts > 1 ? (size_t)(f.tiles - f.whole) * f.parts * f.tm * 32 * 128 * 4 : 0;
+}
+// Whether dY is copied to aligned rows, for the sake of long reductions.  us, copied / any alignment: 11060 x 384 x 8716 171 / 240, 1 x 384 x 10519 16 / 110,
+// 2000 x 4000 x 2001 52 / 91, 2 x 7840 x 655 9.5 / 9.8, 3000 x 1280 x 515 17.2 / 17.7; 5000 x 320 x 260 12 / 8.5, 16384 x 640 x 100 31 / 16, 16 x 1280 x 33 7.5 / 3.5
+// (and 4096 x 1280 x 1283 41 / 37).
+static bool mx_grad_copies(long N) { return N % 8 != 0 && N > 512; }
+size_t mx_grad_workspace_bytes(long M, long N, long K) {
+    return up256(mx_grad_partial_bytes(M, N, K)) + (mx_grad_copies(N) ? (size_t)M * ((N + 7) / 8 * 8) * 2 : 0);
 }
 
 template <int DT, int TM, int NW, int S>
@@ -442,10 +463,17 @@ static int run_mx_grad(const MxGrad& g, const GradForm& f, float* ws, hipStream_
 }
 
 template <int DT>
-static int choose_mx_grad(const MxGrad& g, float* ws, hipStream_t st) {
+static int choose_mx_grad(MxGrad g, float* ws, hipStream_t st) {
     // 32-bit offsets of the loads: a row strip of dY, the weights' codes
-    const bool small = g.lddy < (1 << 22) && (long)g.w.groups * g.w.kc * 1024 < (1L << 31);
-    if (!g.wide || g.N % 8 != 0 || !small) {
+    const bool small = (long)g.w.groups * g.w.kc * 1024 < (1L << 31);
+    if (small && mx_grad_copies(g.N)) {
+        const int ld = (g.N + 7) / 8 * 8;
+        uint16_t* to = (uint16_t*)((char*)ws + up256(mx_grad_partial_bytes(g.M, g.N, g.K)));
+        mx_grad_align_kernel<<<dim3((unsigned)((g.M + 3L) / 4), (unsigned)((g.N + 2047) / 2048)), 256, 0, st>>>(g.dy, g.lddy, g.M, g.N, to, ld);
+        MQ_HIP_CHECK_LAUNCH();
+        g.dy = to, g.lddy = g.N = ld, g.wide = true;
+    }
+    if (!g.wide || g.N % 8 != 0 || !small || g.lddy >= (1 << 22)) {
         mx_grad_any_kernel<DT><<<dim3((unsigned)((g.M + 63L) / 64), (unsigned)g.w.kc), 256, 0, st>>>(g);
         MQ_HIP_CHECK_LAUNCH();
         return MQ_OK;

@@ -319,6 +319,20 @@ def test_linear_grad_views_and_special_values(mq):
     assert np.isnan(dx[7]).all() and np.isnan(dx[:, 32:64]).all() and (dx[3, :32] == 0).all()
 
 
+@pytest.mark.parametrize("M,K,N", ((1, 64, 650), (45, 160, 650), (9, 96, 2100), (300, 352, 1003)))
+def test_linear_grad_rows_copied(mq, M, K, N):
+    """Reductions of any length over rows at any distance: nothing beside a row gets into it."""
+    dy, w = rand((M, N), F16, 24), rand((N, K), F16, 25, 0.05)
+    want = check_grad(mq, dy, w)
+    wq = mq.mx_quantize_weights(w)
+    for pad, offset in ((0, 0), (8, 8), (1, 0), (5, 3)):
+        assert torch.equal(mq.mx_linear_grad(spread(dy, pad, offset), wq), want)
+    if M > 8:
+        dy[4, N - 1], dy[8, 0] = float("nan"), float("inf")
+        dx = f64(check_grad(mq, dy, w))
+        assert np.isnan(dx[4]).all() and np.isfinite(dx[5:8]).all()
+
+
 def test_linear_grad_wants_top(mq):
     with pytest.raises(ValueError):
         mq.mx_linear_grad(rand((2, 8), F16, 1), mq.mx_quantize(rand((8, 64), F16, 1)))

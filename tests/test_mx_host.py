@@ -158,3 +158,9 @@ def test_python_refusals_without_a_gpu(lib):
             call()
     with pytest.raises(TypeError):
         mq.mx_pack(x, x)
+
+
+def test_grad_workspace_of_copied_rows(lib):
+    """Reductions that are no multiple of eight need room for their rows."""
+    need = lambda N: lib.mq_mx_linear_grad_workspace_bytes(300, N, 352)
+    assert need(1003) >= need(1008) + 300 * 1008 * 2 and need(1000) == need(1008)
