@@ -113,8 +113,7 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
 }
 
 // Cache policy of buffer stores: through to memory at once, rather than when the kernel ends and waits for its caches to be written back.  4096 x 1280 x
-// 1280 with a residual 12.5 to 11.3 us, 2964 x 1280 x 3840 16.9 to 13.9, the norm's backward pass over 16384 x 640 two of 30.  Stores by address: the
-// non-temporal kind (dequantising 16384 x 640 0.7 of 11 us).
+// 1280 with a residual 12.5 to 11.3 us, 2964 x 1280 x 3840 16.9 to 13.9, the norm's backward pass over 16384 x 640 two of 30.
 constexpr int WRITE_THROUGH = 17;
 
 // Eight consecutive 16-bit values of a row, of which the first `n` exist (n >= 8: all), wherever they start: the memory takes 16 bytes at any address.
@@ -131,7 +130,7 @@ __device__ __forceinline__ uint4v load8_16(const uint16_t* p, int n) {
 }
 __device__ __forceinline__ void store8_16(uint16_t* p, uint4v v, int n) {
     if (n >= 8) {
-        __builtin_nontemporal_store(v, (uint4v_any*)p);
+        *(uint4v_any*)p = v;
         return;
     }
 #pragma unroll
