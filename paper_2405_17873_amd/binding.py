@@ -737,7 +737,7 @@ def alloc_search(sens_content, params_content, sens_quality, params_quality, bit
 
 # ------------------------------------------- microscaled 4-bit floats, layer norm, and their gradients
 #
-# Matrices are [rows, columns] with contiguous rows, which may lie apart.
+# Matrices are [rows, columns] with contiguous rows, which may lie apart but not over one another (so a broadcast one is made contiguous() first).
 
 
 _HALF = (None, torch.float16)  # mx_linear's default
@@ -757,6 +757,8 @@ class MxTensor:
 
 
 def _matrix(t: torch.Tensor, rows=None, cols=None, dtype=None) -> torch.Tensor:
+    if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"rows overlap: {tuple(t.shape)} with strides {t.stride()}; contiguous() makes a matrix of it")
     if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"expected a matrix on the GPU with contiguous rows, got {tuple(t.shape)} with strides {t.stride()} on {t.device}")
     if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
@@ -772,7 +774,7 @@ def _out(t: Optional[torch.Tensor], rows: int, cols: int, dtype, device) -> torc
 
 def _ld(t: Optional[torch.Tensor]):
     """Row stride; a single row's stride says nothing."""
-    return C.c_long(0 if t is None else max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1])
+    return C.c_long(0 if t is None else t.stride(0) if t.shape[0] > 1 else t.shape[1])
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype, device) -> Optional[torch.Tensor]:

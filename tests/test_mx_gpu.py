@@ -540,3 +540,23 @@ def test_example_tunes_norms(mq):
     spec.loader.exec_module(m)
     losses = m.tune(rows=500, width=160, hidden=608, blocks=2, steps=40, say=lambda *a, **k: None)
     assert all(np.isfinite(losses)) and np.mean(losses[-5:]) < np.mean(losses[:5])
+
+
+# ------------------------------------------------------------------------------------------------------------ refusals
+
+def test_overlapping_rows_are_refused(mq):
+    """A broadcast gradient, rows that lie over one another, as every matrix operand."""
+    M, K, N = 6, 64, 64
+    w = mq.mx_quantize_weights(rand((N, K), F16, 80, 0.05))
+    x = rand((M, K), F16, 81)
+    _, mean, rstd = mq.layer_norm(x, want_stats=True)
+    v = rand((256,), F16, 82)
+    for t in (v[:64].expand(M, K), v.as_strided((M, K), (16, 1))):
+        for call in (lambda: mq.mx_quantize(t), lambda: mq.mx_linear(t, w), lambda: mq.mx_linear(x, w, residual=t), lambda: mq.mx_linear(x, w, out=t),
+                     lambda: mq.mx_linear(mq.mx_quantize(x), w, residual=t), lambda: mq.mx_linear_grad(t, w), lambda: mq.mx_linear_grad(x, w, out=t),
+                     lambda: mq.layer_norm(t), lambda: mq.layer_norm(x, out=t), lambda: mq.layer_norm_mx(t), lambda: mq.layer_norm_grad(t, x, None, mean, rstd),
+                     lambda: mq.layer_norm_grad(x, t, None, mean, rstd), lambda: mq.layer_norm_grad(x, x, None, mean, rstd, residual=t),
+                     lambda: mq.layer_norm_grad(x, x, None, mean, rstd, out=t), lambda: mq.mx_dequantize(w, F16, out=t)):
+            with pytest.raises(ValueError):
+                call()
+        assert torch.equal(mq.mx_linear_grad(t.contiguous(), w), mq.mx_linear_grad(t.clone(memory_format=torch.contiguous_format), w))

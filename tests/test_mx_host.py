@@ -164,3 +164,34 @@ def test_grad_workspace_of_copied_rows(lib):
     """Reductions that are no multiple of eight need room for their rows."""
     need = lambda N: lib.mq_mx_linear_grad_workspace_bytes(300, N, 352)
     assert need(1003) >= need(1008) + 300 * 1008 * 2 and need(1000) == need(1008)
+
+
+def overlapping():
+    """Matrices [4, 64] whose rows lie on or over one another: a broadcast row, and rows 16 values apart."""
+    import torch
+    v = torch.zeros(256, dtype=torch.float16)
+    return v[:64].expand(4, 64), v.as_strided((4, 64), (16, 1))
+
+
+def test_row_strides_are_the_tensors_own(lib):
+    """A stride below the row reaches the entry points as it is, which refuse it: a larger one would have them read past the allocation."""
+    import torch
+
+    from paper_2405_17873_amd import binding
+    assert [binding._ld(t).value for t in overlapping()] == [0, 16]
+    assert binding._ld(torch.zeros(4, 80)[:, :64]).value == 80
+    assert binding._ld(torch.zeros(1, 64).as_strided((1, 64), (7, 1))).value == 64  # a single row's stride says nothing
+    assert binding._ld(torch.zeros(0, 64)).value == 64
+
+
+def test_overlapping_rows_are_refused(lib):
+    import torch
+
+    import paper_2405_17873_amd as mq
+    w = mq.MxTensor(torch.zeros(mq.mx_bytes(64, 64), dtype=torch.uint8), 64, 64, torch.zeros(2, dtype=torch.uint8))
+    stats = torch.zeros(4)
+    for t in overlapping():
+        for call in (lambda: mq.mx_quantize(t), lambda: mq.mx_linear(t, w), lambda: mq.mx_linear_grad(t, w), lambda: mq.layer_norm(t), lambda: mq.layer_norm_mx(t),
+                     lambda: mq.mx_dequantize(w, torch.float16, out=t), lambda: mq.layer_norm_grad(t, t, None, stats, stats)):
+            with pytest.raises(ValueError, match="overlap"):
+                call()
