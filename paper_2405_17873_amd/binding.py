@@ -756,20 +756,22 @@ class MxTensor:
         return (self.rows, self.K)
 
 
-def _matrix(t: torch.Tensor, rows=None, cols=None, dtype=None) -> torch.Tensor:
+def _matrix(t: torch.Tensor, rows=None, cols=None, dtype=None, device=None) -> torch.Tensor:
     if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
         raise ValueError(f"rows overlap: {tuple(t.shape)} with strides {t.stride()}; contiguous() makes a matrix of it")
     if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"expected a matrix on the GPU with contiguous rows, got {tuple(t.shape)} with strides {t.stride()} on {t.device}")
     if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
         raise ValueError(f"expected [{rows}, {cols}], got {tuple(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"expected a matrix on {device}, got one on {t.device}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
     return t
 
 
 def _out(t: Optional[torch.Tensor], rows: int, cols: int, dtype, device) -> torch.Tensor:
-    return torch.empty((rows, cols), dtype=dtype, device=device) if t is None else _matrix(t, rows, cols, dtype)
+    return torch.empty((rows, cols), dtype=dtype, device=device) if t is None else _matrix(t, rows, cols, dtype, device)
 
 
 def _ld(t: Optional[torch.Tensor]):
@@ -785,6 +787,22 @@ def _vector(t: Optional[torch.Tensor], n: int, dtype, device) -> Optional[torch.
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
     return t
+
+
+def _mx_data(t: MxTensor, device=None):
+    """Address of a microscaled matrix, which may have been made or moved by hand."""
+    d, need = t.data, mx_bytes(t.rows, t.K)
+    if d.dtype != torch.uint8 or not d.is_contiguous() or d.numel() < need:
+        raise ValueError(f"a microscaled matrix of {t.rows} x {t.K} has {need} contiguous bytes, got {d.numel()} of {d.dtype} with strides {d.stride()}")
+    if not d.is_cuda or (device is not None and d.device != device):
+        raise ValueError(f"expected a microscaled matrix on {device or 'the GPU'}, got one on {d.device}")
+    return _ptr(d)
+
+
+def _mx_workspace(nbytes: int, device, ws: Optional[torch.Tensor]) -> torch.Tensor:
+    if ws is not None and (ws.device != device or not ws.is_contiguous()):
+        raise ValueError(f"expected a contiguous workspace on {device}, got one on {ws.device} with strides {ws.stride()}")
+    return _workspace(nbytes, device, ws)
 
 
 def _bytes_of(ws: torch.Tensor):
@@ -820,8 +838,9 @@ def mx_quantize_weights(w: torch.Tensor) -> MxTensor:
 
 
 def _with_top(t: MxTensor) -> MxTensor:
+    data = _mx_data(t)
     t.top = torch.empty(t.K // 32, dtype=torch.uint8, device=t.data.device)
-    _check(load().mq_mx_column_top(_ptr(t.data), t.rows, t.K, _ptr(t.top), _stream()), "mq_mx_column_top")
+    _check(load().mq_mx_column_top(data, t.rows, t.K, _ptr(t.top), _stream()), "mq_mx_column_top")
     return t
 
 
@@ -832,7 +851,7 @@ def mx_dequantize(t: MxTensor, dtype=torch.bfloat16, out: Optional[torch.Tensor]
         if r is not None:
             return _done(r, "mq_mx_dequantize")
     y = _out(out, t.rows, t.K, dtype, t.data.device)
-    _check(load().mq_mx_dequantize(_ptr(t.data), t.rows, t.K, _dtype_code(y), _ptr(y), _ld(y), _stream()), "mq_mx_dequantize")
+    _check(load().mq_mx_dequantize(_mx_data(t), t.rows, t.K, _dtype_code(y), _ptr(y), _ld(y), _stream()), "mq_mx_dequantize")
     return y
 
 
@@ -850,9 +869,10 @@ def mx_pack(codes: torch.Tensor, scales: torch.Tensor) -> MxTensor:
 
 def mx_unpack(t: MxTensor):
     """(codes uint8 [M, K/2], scales uint8 [M, K/32])."""
+    data = _mx_data(t)
     codes = torch.empty((t.rows, t.K // 2), dtype=torch.uint8, device=t.data.device)
     scales = torch.empty((t.rows, t.K // 32), dtype=torch.uint8, device=t.data.device)
-    _check(load().mq_mx_unpack(_ptr(t.data), t.rows, t.K, _ptr(codes), _ptr(scales), _stream()), "mq_mx_unpack")
+    _check(load().mq_mx_unpack(data, t.rows, t.K, _ptr(codes), _ptr(scales), _stream()), "mq_mx_unpack")
     return codes, scales
 
 
@@ -890,13 +910,13 @@ def mx_linear(x: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[torc
     y = _out(out, M, w.rows, dtype, device)
     dt = _dtype_code(y)
     if residual is not None:
-        _matrix(residual, M, w.rows, dtype)
-    args = (_ptr(w.data), w.rows, _ptr(_vector(bias, w.rows, dtype, device)), _ptr(y), _ld(y), dt, _ptr(residual), _ld(residual))
+        _matrix(residual, M, w.rows, dtype, device)
+    args = (_mx_data(w, device), w.rows, _ptr(_vector(bias, w.rows, dtype, device)), _ptr(y), _ld(y), dt, _ptr(residual), _ld(residual))
     if packed:
-        _check(lib.mq_mx_linear_codes(_ptr(x.data), M, K, *args, _stream()), "mq_mx_linear_codes")
+        _check(lib.mq_mx_linear_codes(_mx_data(x, device), M, K, *args, _stream()), "mq_mx_linear_codes")
     else:
-        if ws is None:  # (a few rows do without, unless the output lies over them)
-            ws = torch.empty(mx_linear_workspace_bytes(M, w.rows, K) if out is None else mx_bytes(M, K), dtype=torch.uint8, device=device)
+        # (a few rows do without, unless the output lies over them)
+        ws = _mx_workspace(mx_linear_workspace_bytes(M, w.rows, K) if out is None else mx_bytes(M, K), device, ws)
         _check(lib.mq_mx_linear(_ptr(x), M, K, _ld(x), *args, _ptr(ws), _bytes_of(ws), _stream()), "mq_mx_linear")
     return y
 
@@ -916,8 +936,9 @@ def mx_linear_grad(dy: torch.Tensor, w: MxTensor, out: Optional[torch.Tensor] = 
             return _done(r, "mq_mx_linear_grad")
     M, N = _matrix(dy, cols=w.rows).shape
     dx = _out(out, M, w.K, dy.dtype, dy.device)
-    ws = _workspace(mx_linear_grad_workspace_bytes(M, N, w.K), dy.device, ws)
-    _check(load().mq_mx_linear_grad(_ptr(dy), M, N, _ld(dy), _ptr(w.data), _ptr(w.top), w.K, _ptr(dx), _ld(dx), _dtype_code(dy), *_ws_args(ws),
+    ws = _mx_workspace(mx_linear_grad_workspace_bytes(M, N, w.K), dy.device, ws)
+    top = _vector(w.top, w.K // 32, torch.uint8, dy.device)
+    _check(load().mq_mx_linear_grad(_ptr(dy), M, N, _ld(dy), _mx_data(w, dy.device), _ptr(top), w.K, _ptr(dx), _ld(dx), _dtype_code(dy), *_ws_args(ws),
                                     _stream()), "mq_mx_linear_grad")
     return dx
 
@@ -983,15 +1004,15 @@ def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Te
         if r is not None:
             return _done(r, "mq_layer_norm_grad")
     M, N = _matrix(x).shape
-    _matrix(dy, M, N, x.dtype)
+    _matrix(dy, M, N, x.dtype, x.device)
     if residual is not None:
-        _matrix(residual, M, N, x.dtype)
+        _matrix(residual, M, N, x.dtype, x.device)
     w, _, pt = _params(x, weight, None)
     _vector(mean, M, torch.float32, x.device)
     _vector(rstd, M, torch.float32, x.device)
     dx = _out(out, M, N, x.dtype, x.device)
     sums = torch.empty((2, N), dtype=torch.float32, device=x.device)
-    ws = _workspace(layer_norm_grad_workspace_bytes(M, N), x.device, ws)
+    ws = _mx_workspace(layer_norm_grad_workspace_bytes(M, N), x.device, ws)
     _check(load().mq_layer_norm_grad(_ptr(dy), _ld(dy), _ptr(x), _ld(x), M, N, _ptr(w), pt, _ptr(mean), _ptr(rstd), _ptr(residual), _ld(residual),
                                      _ptr(dx), _ld(dx), _dtype_code(x), _ptr(sums[0]), _ptr(sums[1]), _ptr(ws), _bytes_of(ws), _stream()),
            "mq_layer_norm_grad")

@@ -316,10 +316,10 @@ bool matrix(PyObject* o, Matrix& m) {
     m.p = m.t->data_ptr();
     return m.dtype >= 0 && m.rows > 0 && m.cols > 0 && (m.cols == 1 || m.t->stride(1) == 1) && m.ld >= m.cols;
 }
-// The same as an optional operand of a given size and type: all zero for None.
-bool optional_matrix(PyObject* o, int rows, int cols, int dtype, Matrix& m) {
+// The same as an optional operand of a given size, type and device: all zero for None.
+bool optional_matrix(PyObject* o, int rows, int cols, int dtype, at::Device device, Matrix& m) {
     m = Matrix{};
-    return o == Py_None || (matrix(o, m) && m.rows == rows && m.cols == cols && m.dtype == dtype);
+    return o == Py_None || (matrix(o, m) && m.rows == rows && m.cols == cols && m.dtype == dtype && m.t->device() == device);
 }
 // An optional contiguous vector of n on x's device (its type in *type).
 bool vector(PyObject* o, int64_t n, at::Device device, void*& p, at::ScalarType* type) {
@@ -330,10 +330,11 @@ bool vector(PyObject* o, int64_t n, at::Device device, void*& p, at::ScalarType*
     *type = t->scalar_type();
     return true;
 }
-// A microscaled buffer of rows x K: its address, or false.
-bool mx_data(PyObject* o, int rows, int K, void*& p) {
+// A microscaled buffer of rows x K (on the device of another operand): its address, or false.
+bool mx_data(PyObject* o, int rows, int K, void*& p, const at::Tensor* beside = nullptr) {
     const at::Tensor* t = gpu_tensor(o);
-    if (!t || rows <= 0 || K <= 0 || t->scalar_type() != at::kByte || t->nbytes() < entry.mx_bytes(rows, K)) return false;
+    if (!t || rows <= 0 || K <= 0 || t->scalar_type() != at::kByte || !t->is_contiguous() || t->nbytes() < entry.mx_bytes(rows, K)) return false;
+    if (beside && t->device() != beside->device()) return false;
     p = t->data_ptr();
     return true;
 }
@@ -400,11 +401,12 @@ PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
         Matrix x, res;
         int N, K;
         void *w, *bias;
-        if (n != 6 || !plain_calls() || !matrix(a[0], x) || !small_int(a[2], N) || !small_int(a[3], K) || x.cols != K || !mx_data(a[1], N, K, w))
+        if (n != 6 || !plain_calls() || !matrix(a[0], x) || !small_int(a[2], N) || !small_int(a[3], K) || x.cols != K ||
+            !mx_data(a[1], N, K, w, x.t))
             return general();
         const at::Device device = x.t->device();
         at::ScalarType type = x.t->scalar_type();
-        if (!vector(a[4], N, device, bias, &type) || type != x.t->scalar_type() || !optional_matrix(a[5], x.rows, N, x.dtype, res)) return general();
+        if (!vector(a[4], N, device, bias, &type) || type != x.t->scalar_type() || !optional_matrix(a[5], x.rows, N, x.dtype, device, res)) return general();
         at::Tensor y, ws;
         int rc;
         {
@@ -428,12 +430,12 @@ PyObject* mx_linear_codes(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int M, K, N, dtype;
         void *x, *w, *bias;
         if (n != 8 || !plain_calls() || !small_int(a[1], M) || !small_int(a[2], K) || !small_int(a[4], N) || !small_int(a[7], dtype) ||
-            (dtype != 0 && dtype != 1) || !mx_data(a[0], M, K, x) || !mx_data(a[3], N, K, w))
+            (dtype != 0 && dtype != 1) || !mx_data(a[0], M, K, x) || !mx_data(a[3], N, K, w, gpu_tensor(a[0])))
             return general();
         const at::Device device = gpu_tensor(a[0])->device();
         const at::ScalarType want = dtype ? at::kBFloat16 : at::kHalf;
         at::ScalarType type = want;
-        if (!vector(a[5], N, device, bias, &type) || type != want || !optional_matrix(a[6], M, N, dtype, res)) return general();
+        if (!vector(a[5], N, device, bias, &type) || type != want || !optional_matrix(a[6], M, N, dtype, device, res)) return general();
         at::Tensor y;
         int rc;
         {
@@ -455,8 +457,8 @@ PyObject* mx_linear_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int N, K;
         void* w;
         const at::Tensor* top;
-        if (n != 5 || !plain_calls() || !matrix(a[0], dy) || !small_int(a[2], N) || !small_int(a[3], K) || dy.cols != N || !mx_data(a[1], N, K, w) ||
-            !(top = gpu_tensor(a[4])) || top->scalar_type() != at::kByte || !top->is_contiguous() || top->numel() != K / 32)
+        if (n != 5 || !plain_calls() || !matrix(a[0], dy) || !small_int(a[2], N) || !small_int(a[3], K) || dy.cols != N || !mx_data(a[1], N, K, w, dy.t) ||
+            !(top = gpu_tensor(a[4])) || top->scalar_type() != at::kByte || !top->is_contiguous() || top->numel() != K / 32 || top->device() != dy.t->device())
             return general();
         const void* tp = top->data_ptr();
         const at::Device device = dy.t->device();
@@ -530,7 +532,7 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (n != 6 || !plain_calls() || !matrix(a[1], x) || !matrix(a[0], dy) || dy.rows != x.rows || dy.cols != x.cols || dy.dtype != x.dtype ||
             !norm_params(a[2], Py_None, x, w, b, pt) || !vector(a[3], x.rows, x.t->device(), mean, &tm) ||
             !vector(a[4], x.rows, x.t->device(), rstd, &tr) || !mean || !rstd || tm != at::kFloat || tr != at::kFloat ||
-            !optional_matrix(a[5], x.rows, x.cols, x.dtype, res))
+            dy.t->device() != x.t->device() || !optional_matrix(a[5], x.rows, x.cols, x.dtype, x.t->device(), res))
             return general();
         const at::Device device = x.t->device();
         at::Tensor dx, dw, db, ws;

@@ -560,3 +560,30 @@ def test_overlapping_rows_are_refused(mq):
             with pytest.raises(ValueError):
                 call()
         assert torch.equal(mq.mx_linear_grad(t.contiguous(), w), mq.mx_linear_grad(t.clone(memory_format=torch.contiguous_format), w))
+
+
+def test_buffers_are_looked_at(mq):
+    """Microscaled matrices, column scales and workspaces on the host, too short, of another type or not contiguous: the call raises instead of launching."""
+    import dataclasses
+    M, K, N = 5, 64, 64
+    w, x = mq.mx_quantize_weights(rand((N, K), F16, 80, 0.05)), rand((M, K), F16, 81)
+    xq, (_, mean, rstd), n = mq.mx_quantize(x), mq.layer_norm(x, want_stats=True), mq.mx_bytes(N, K)
+    part = torch.zeros(2 * n, dtype=torch.uint8, device="cuda")
+    for data in (w.data.cpu(), w.data[:n - 1], w.data.view(torch.int8), part[::2], part[:1].expand(n)):
+        t = dataclasses.replace(w, data=data)
+        for call in (lambda: mq.mx_linear(x, t), lambda: mq.mx_linear(x, t, out=torch.empty_like(x)), lambda: mq.mx_linear(xq, t), lambda: mq.mx_linear(t, w),
+                     lambda: mq.mx_linear_grad(x, t), lambda: mq.mx_linear_grad(x, t, out=torch.empty_like(x)), lambda: mq.mx_dequantize(t),
+                     lambda: mq.mx_dequantize(t, out=torch.empty(N, K, dtype=BF16, device="cuda")), lambda: mq.mx_unpack(t)):
+            with pytest.raises(ValueError):
+                call()
+    for top, error in ((w.top.cpu(), ValueError), (w.top[:1], ValueError), (w.top.to(torch.int8), TypeError), (part[::2][:2], ValueError)):
+        with pytest.raises(error):
+            mq.mx_linear_grad(x, dataclasses.replace(w, top=top))
+    for ws in (torch.zeros(1 << 20, dtype=torch.uint8), torch.zeros(1 << 21, dtype=torch.uint8, device="cuda")[::2]):
+        for call in (lambda: mq.mx_linear(x, w, ws=ws), lambda: mq.mx_linear_grad(x, w, ws=ws), lambda: mq.layer_norm_grad(x, x, None, mean, rstd, ws=ws)):
+            with pytest.raises(ValueError):
+                call()
+    for call in (lambda: mq.mx_linear(x, w, residual=x.cpu()), lambda: mq.mx_linear(x, w, out=x.cpu()), lambda: mq.layer_norm_grad(x.cpu(), x, None, mean, rstd),
+                 lambda: mq.layer_norm_grad(x, x, None, mean.cpu(), rstd)):
+        with pytest.raises(ValueError):
+            call()

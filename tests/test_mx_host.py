@@ -195,3 +195,29 @@ def test_overlapping_rows_are_refused(lib):
                      lambda: mq.mx_dequantize(w, torch.float16, out=t), lambda: mq.layer_norm_grad(t, t, None, stats, stats)):
             with pytest.raises(ValueError, match="overlap"):
                 call()
+
+
+def test_buffers_are_looked_at(lib):
+    """What a microscaled matrix carries, its column scales and workspaces: on the host, too short, of another type or not contiguous."""
+    import dataclasses
+
+    import torch
+
+    import paper_2405_17873_amd as mq
+    from paper_2405_17873_amd import binding
+    n = mq.mx_bytes(64, 64)
+    on_host = mq.MxTensor(torch.zeros(n, dtype=torch.uint8), 64, 64, torch.zeros(2, dtype=torch.uint8))
+    bad = [on_host] + [dataclasses.replace(on_host, data=d) for d in (torch.zeros(n - 1, dtype=torch.uint8), torch.zeros(n, dtype=torch.int8),
+                                                                     torch.zeros(1, dtype=torch.uint8).expand(n), torch.zeros(2 * n, dtype=torch.uint8)[::2])]
+    for t in bad:
+        for call in (lambda: mq.mx_dequantize(t), lambda: mq.mx_unpack(t), lambda: mq.mx_linear(t, on_host), lambda: binding._with_top(t)):
+            with pytest.raises(ValueError):
+                call()
+    for t, what in zip(bad, ("on", "bytes", "bytes", "bytes", "bytes")):
+        with pytest.raises(ValueError, match=what):
+            binding._mx_data(t)
+    cpu = torch.device("cpu")
+    for ws in (torch.zeros(512, dtype=torch.uint8)[::2], torch.zeros(1, dtype=torch.uint8).expand(512), torch.zeros(512, dtype=torch.uint8, device="meta")):
+        with pytest.raises(ValueError):
+            binding._mx_workspace(256, cpu, ws)
+    assert binding._mx_workspace(256, cpu, None).numel() == 256
