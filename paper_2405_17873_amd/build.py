@@ -37,7 +37,7 @@ SOURCES = ["api.hip", "quant_pack.hip", "act_quant.hip", "gemm.hip", "gemm_solo.
 def _compile(src: str, force: bool) -> str:
     path = os.path.join(CSRC, src)
     obj = os.path.join(OBJ, src + ".o")
-    deps = [path, os.path.join(CSRC, "mq_common.h"), os.path.join(CSRC, "bos_rows.h"), os.path.join(CSRC, "gemm_core.h"), os.path.join(CSRC, "act_range.h"), os.path.join(CSRC, "mx_common.h"),
+    deps = [path, os.path.join(CSRC, "mq_common.h"), os.path.join(CSRC, "bos_rows.h"), os.path.join(CSRC, "gemm_core.h"), os.path.join(CSRC, "act_range.h"), os.path.join(CSRC, "mx_common.h"), os.path.join(CSRC, "per_device.h"),
             os.path.join(HERE, "..", "include", "mixdq.h"), __file__]
     if not force and os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
         return obj

@@ -13,6 +13,7 @@
 // their byte of it.  Rows are padded to 32, columns to 64 (scales to 256): padding holds code 0, scale 0, and so adds nothing to a product.
 #pragma once
 #include "gemm_core.h"
+#include "per_device.h"
 
 namespace mq {
 
@@ -141,6 +142,17 @@ __device__ __forceinline__ void store8_16(uint16_t* p, uint4v v, int n) {
 }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+// Allows a kernel more than 64 KB of dynamic LDS on the current device.  `prepared`: the kernel's own.
+inline int allow_lds(PerDevice& prepared, const void* kernel, int bytes) {
+    int device = -1;
+    if (hipGetDevice(&device) != hipSuccess) device = -1;
+    return prepared(device, [&]() -> int {
+        if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) return MQ_OK;
+        set_hip_error((int)hipGetLastError());
+        return MQ_ERR_HIP;
+    });
+}
 
 // ---- launchers (arguments are checked by the entry points) ----
 struct MxGemm {

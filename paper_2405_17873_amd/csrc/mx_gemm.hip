@@ -351,11 +351,8 @@ static int run_mx_form(const MxGemm& g, long band, long most, hipStream_t st) {
     using P = MxPlan<WM, WN, TM, TN, S>;
     const long rows = (g.a.groups + P::GA - 1) / P::GA, cols = (g.w.groups + P::GB - 1) / P::GB;
     auto kernel = mx_gemm_kernel<DT, EPI, WM, WN, TM, TN, S>;
-    static const hipError_t set = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, P::BYTES);
-    if (set != hipSuccess) {
-        set_hip_error((int)set);
-        return MQ_ERR_HIP;
-    }
+    static PerDevice prepared;
+    if (const int rc = allow_lds(prepared, (const void*)kernel, P::BYTES)) return rc;
     // (several tiles for a workgroup: where a tile has at least as many steps as there are slots)
     const long wgs = rows * cols <= most || (g.a.kc + 1) / 2 < S ? rows * cols : most;
     kernel<<<(unsigned)wgs, P::NW * 64, P::BYTES, st>>>(g, mx_tiles(rows, cols, band));

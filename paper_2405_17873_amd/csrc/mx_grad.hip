@@ -442,11 +442,8 @@ static int run_mx_grad(const MxGrad& g, const GradForm& f, float* ws, hipStream_
     using P = GradPlan<TM, NW, S>;
     static_assert(P::BYTES <= 160 * 1024, "LDS of a compute unit");
     auto kernel = mx_grad_kernel<DT, TM, NW, S>;
-    static const hipError_t set = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, P::BYTES);
-    if (set != hipSuccess) {
-        set_hip_error((int)set);
-        return MQ_ERR_HIP;
-    }
+    static PerDevice prepared;
+    if (const int rc = allow_lds(prepared, (const void*)kernel, P::BYTES)) return rc;
     GradWork w;
     w.col_tiles = (uint32_t)((g.K / 32 + 3) / 4);
     w.whole = (uint32_t)f.whole;

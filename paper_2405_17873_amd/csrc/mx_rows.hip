@@ -139,11 +139,8 @@ template <int DT, bool MXIN, int RG, int U>
 static int run_mx_rows(const MxRows& r, hipStream_t st) {
     constexpr int BYTES = 8 * RG * 32 * (32 + 4) * 4;
     auto kernel = mx_rows_kernel<DT, MXIN, RG, U>;
-    static const hipError_t set = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, BYTES);
-    if (set != hipSuccess) {
-        set_hip_error((int)set);
-        return MQ_ERR_HIP;
-    }
+    static PerDevice prepared;
+    if (const int rc = allow_lds(prepared, (const void*)kernel, BYTES)) return rc;
     kernel<<<(unsigned)r.g.w.groups, 512, BYTES, st>>>(r);
     MQ_HIP_CHECK_LAUNCH();
     return MQ_OK;

@@ -221,3 +221,33 @@ def test_buffers_are_looked_at(lib):
         with pytest.raises(ValueError):
             binding._mx_workspace(256, cpu, ws)
     assert binding._mx_workspace(256, cpu, None).numel() == 256
+
+
+def test_once_per_device(tmp_path):
+    """What kernels with much LDS are prepared with: done on every device, once, and again after a failure."""
+    import re
+    import subprocess
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2405_17873_amd", "csrc")
+    (tmp_path / "t.cpp").write_text("""
+#include <stdio.h>
+#include "per_device.h"
+int main() {
+    static mq::PerDevice prepared;
+    int calls = 0, fail = 0;
+    auto f = [&] { ++calls; return fail; };
+    for (int d : {0, 0, 1, 0, 1, 15}) prepared(d, f);
+    printf("%d ", calls);
+    fail = 7;
+    const int a = prepared(2, f), b = prepared(2, f), c = prepared(0, f);
+    fail = 0;
+    const int d = prepared(2, f), e = prepared(2, f);
+    printf("%d %d %d %d %d %d ", calls, a, b, c, d, e);
+    prepared(99, f), prepared(99, f), prepared(-1, f);
+    printf("%d", calls);
+}""")
+    subprocess.run(["g++", "-std=c++17", "-I", csrc, str(tmp_path / "t.cpp"), "-o", str(tmp_path / "t"), "-pthread"], check=True)
+    assert subprocess.run([str(tmp_path / "t")], check=True, capture_output=True, text=True).stdout.split() == "3 6 7 7 0 0 0 9".split()
+    for name in sorted(os.listdir(csrc)):
+        if name.startswith("mx_"):
+            for line in open(os.path.join(csrc, name)):
+                assert not re.search(r"static\s+const\s+hipError_t", line), f"{name} keeps one device's answer for all: {line}"
