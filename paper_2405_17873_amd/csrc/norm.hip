@@ -161,8 +161,9 @@ __global__ __launch_bounds__(256) void layer_norm_kernel(const NormArgs g, const
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += v[i][e];
     }
-    const float inv = 1.0f / (float)g.C;
-    const float mean = row_sum<LPR>(s, slot) * inv;
+    // (Divided, not multiplied by 1 / C: the mean of a row of equal values, whose sum is exact, is then that value, and nothing is left of the row.)
+    const float cols = (float)g.C;
+    const float mean = row_sum<LPR>(s, slot) / cols;
     float q = 0.0f;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
@@ -173,7 +174,7 @@ __global__ __launch_bounds__(256) void layer_norm_kernel(const NormArgs g, const
             q += e < n ? v[i][e] * v[i][e] : 0.0f;
         }
     }
-    const float rstd = 1.0f / sqrtf(row_sum<LPR>(q, slot) * inv + g.eps);
+    const float rstd = 1.0f / sqrtf(row_sum<LPR>(q, slot) / cols + g.eps);
     if (real && li == 0) {
         if (g.mean) g.mean[row] = mean;
         if (g.rstd) g.rstd[row] = rstd;
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormArgs g) 
     constexpr int RPW = 256 / LPR, COLS = LPR * VPT * 8;
     __shared__ __attribute__((aligned(16))) float sums[LPR < 256 ? RPW * COLS : 4];  // LPR == 256: for row_sum
     const int li = threadIdx.x % LPR, ri = threadIdx.x / LPR;
-    const float inv = 1.0f / (float)g.C;
+    const float cols = (float)g.C;
     float aw[VPT][8], ab[VPT][8];
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
@@ -342,8 +343,8 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormArgs g) 
             }
         }
         if (WIDE && row0 + stride < g.M) load(row0 + stride);
-        s1 = row_sum<LPR>(s1, sums) * inv;
-        s2 = row_sum<LPR>(s2, sums) * inv;
+        s1 = row_sum<LPR>(s1, sums) / cols;
+        s2 = row_sum<LPR>(s2, sums) / cols;
         const long rows = rows_at(row0);
         const Rows<WIDE> dx(g.dx, g.lddx, row0, rows, g.C);
 #pragma unroll

@@ -587,3 +587,22 @@ def test_buffers_are_looked_at(mq):
                  lambda: mq.layer_norm_grad(x, x, None, mean.cpu(), rstd)):
         with pytest.raises(ValueError):
             call()
+
+
+# ---------------------------------------------------------------------------------------------- norms: rows without variance, far values
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C", (3, 96, 320, 333, 448, 640, 896, 1000, 1001, 1120, 2709, 4099, 8191))
+def test_layer_norm_constant_rows(mq, C, dtype):
+    """Rows of one value: up to 2^13 of 11 significant bits add up exactly in float32 in any order, so the mean is the value, what is left of the row
+    is zero, and the output is the bias; likewise the gradient of a constant dY, which is zero."""
+    x = torch.tensor([1000.0, 60000.0, 0.1, -7.7, 3e-5, 1.0 / 3.0, -65504.0], dtype=dtype, device="cuda").view(-1, 1).repeat(1, C)
+    w, b = params(C, "f32", dtype, 90)
+    y, mean, rstd = mq.layer_norm(x, w, b, 1e-5, want_stats=True)
+    assert torch.equal(mean, x[:, 0].float())
+    assert torch.equal(y, b.to(dtype).expand_as(y))
+    dx, dw, _ = mq.layer_norm_grad(x, x, None, mean, rstd)
+    assert not dx.any() and not dw.any()
+    if C % 32 == 0:
+        v = mq.mx_dequantize(mq.layer_norm_mx(x, w, b, 1e-5), BF16)
+        assert np.array_equal(f64(v), np.repeat(omx.values(f64(b)[None]), len(x), 0))
