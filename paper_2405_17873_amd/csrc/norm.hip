@@ -334,7 +334,7 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormArgs g) 
             weight.template get<DT>(i, k, n, 1.0f, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                xh[i][e] = (xh[i][e] - m) * r;
+                xh[i][e] = (WIDE ? n > 0 : e < n) ? (xh[i][e] - m) * r : 0.0f;  // (a far mean over a small variance passes fp32's range)
                 gr[i][e] = WIDE || e < n ? d[e] * w[e] : 0.0f;
                 aw[i][e] += d[e] * xh[i][e];
                 ab[i][e] += d[e];

@@ -606,3 +606,22 @@ def test_layer_norm_constant_rows(mq, C, dtype):
     if C % 32 == 0:
         v = mq.mx_dequantize(mq.layer_norm_mx(x, w, b, 1e-5), BF16)
         assert np.array_equal(f64(v), np.repeat(omx.values(f64(b)[None]), len(x), 0))
+
+
+@pytest.mark.parametrize("C", (8, 24, 33, 328, 1288, 4104))
+def test_layer_norm_grad_far_mean(mq, C):
+    """Means near the end of bfloat16's range under small variances: lanes that have no columns must not turn 0 times infinity into the row's sum."""
+    M = 3
+    x = torch.full((M, C), 1e37, dtype=BF16, device="cuda")
+    dy, res = rand((M, C), BF16, 91), rand((M, C), BF16, 92)
+    for kind in ("16", "none"):
+        w, _ = params(C, kind, BF16, 93)
+        mean, rstd = x[:, 0].float().contiguous(), torch.full((M,), 316.0, device="cuda")
+        dx, dw, db = mq.layer_norm_grad(dy, x, w, mean, rstd, residual=res)
+        g = f64(dy) * (1.0 if w is None else f64(w))
+        want = 316.0 * (g - g.mean(-1, keepdims=True)) + f64(res)  # xhat is zero
+        m1 = np.abs(g).mean(-1, keepdims=True)
+        err = 316.0 * (6 * U * (np.abs(g) + m1) + (depth(C) + 4) * U * m1) + 2 * U * np.abs(f64(res)) + 2 * U * np.abs(want)
+        within(f64(dx), want, err + half_step(np.abs(want) + err, BF16))
+        assert not dw.any()
+        within(f64(db), f64(dy).sum(0), (M + 70) * U * np.abs(f64(dy)).sum(0))
