@@ -438,7 +438,8 @@ int mq_mx_linear_codes(const void* a, int M, int K, const void* w, int N, const 
                        void* stream);
 
 /* Gradient of mq_mx_linear with respect to X, the quantisation of X passed straight through: dX = dY W, dY [M,N], dX [M,K] of dtype, sums fp32,
- * rounded once.  top: mq_mx_column_top of W.  Weights below 2^-37 (bfloat16: 2^-128) of the largest of their block column may be taken as zero. */
+ * rounded once.  top: mq_mx_column_top of W.  fp16: weights below 2^-37 of the largest of their block column may be taken as zero.  bfloat16:
+ * weights count as they are (beside scales past 252, which mq_mx_quantize does not make, those of 0 and 1 up to fourfold: 2^-250 of the largest). */
 size_t mq_mx_linear_grad_workspace_bytes(int M, int N, int K); /* 0: none is needed, ws may be null */
 int mq_mx_linear_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* ws,
                       size_t ws_bytes, void* stream);

@@ -1,9 +1,10 @@
 // Gradient of a microscaled 4-bit linear with respect to its input: dX = dY W, the 4-bit weights widened to 16 bits on their way into the MFMAs.
 //
 // The reduction runs over the weights' rows n, along which neither codes nor scales are contiguous.  Widened 16-bit rows of k go to LDS and come back
-// through the transposing LDS load, which hands a lane consecutive n of one column k.  Widened weights are taken relative to the largest scale of
-// their block column (top): fp16 has too few exponents for 2^(s - 127), and a value 2^-37 of its column's largest may go.  The product is scaled
-// back at the end, exactly.
+// through the transposing LDS load, which hands a lane consecutive n of one column k.  In fp16, which has too few exponents for 2^(s - 127), widened
+// weights are taken relative to the largest scale of their block column (top), and a value 2^-37 of its column's largest may go; the product is scaled
+// back at the end, exactly.  bfloat16 has the exponents, and weights go in as they are: relative ones of ordinary layers were larger, and sums of a dY
+// near the end of its range became infinite on the way to finite results.
 #include "mx_common.h"
 
 namespace mq {
@@ -25,12 +26,14 @@ struct MxGrad {
     bool wide;  // rows of dY start on 16-byte boundaries
 };
 
-// Exponent field that a block with the largest scale of its column is widened with: 6 units are then 49152 in fp16, 1.5 in bfloat16.
+// What is added to the scale bytes of a block column with the largest scale `top`, and taken back at the end.  fp16: 6 units of the largest are 49152.
+// bfloat16: nothing, but that products of columns below 2^-60 keep clear of the subnormal floats, and that 6 units of the largest are a bfloat16 (beside
+// scales past 252, which no quantiser makes, those of 0 and 1 count up to fourfold then; a mask of their codes costs 8192 x 8192 x 8192 1030 -> 1045 us).
 template <int DT>
-constexpr int mx_grad_field() {
-    return DT == MQ_F16 ? 140 : 125;
+__device__ __forceinline__ int mx_grad_shift(int top) {
+    return DT == MQ_F16 ? 140 - top : top < 64 ? 64 - top : top > 252 ? 252 - top : 0;
 }
-// Scale operand of a block: scale byte s, `shift` = field - top of its column.
+// Scale operand of a block with scale byte s.  (Exponent field 0 and below: nothing that fp16 holds.)
 __device__ __forceinline__ float mx_grad_scale(uint32_t s, int shift) {
     const int f = (int)s + shift;
     return mx_scale_operand(s == 255u ? 255u : f > 0 ? (uint32_t)f : 0u);
@@ -57,7 +60,7 @@ __device__ __forceinline__ float16v mx_grad_mfma(uint4v w, uint4v d, float16v c)
 // Eight sums of a block column, scaled back and rounded.
 template <int DT>
 __device__ __forceinline__ uint4v mx_grad_result(float4v a, float4v b, int top) {
-    const int back = top - mx_grad_field<DT>();
+    const int back = -mx_grad_shift<DT>(top);
     return uint4v{T16<DT>::pack(ldexpf(a[0], back), ldexpf(a[1], back)), T16<DT>::pack(ldexpf(a[2], back), ldexpf(a[3], back)),
                   T16<DT>::pack(ldexpf(b[0], back), ldexpf(b[1], back)), T16<DT>::pack(ldexpf(b[2], back), ldexpf(b[3], back))};
 }
@@ -166,7 +169,7 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
     // widening: the lane has row wn (of 16) of block wb; its four pieces of eight columns lie at p ^ turned(wn)
     const int wn = lane & 15, wb = lane >> 4;
     const int b_mine = b0 + wb < blocks ? b0 + wb : blocks - 1;
-    const int shift = mx_grad_field<DT>() - (int)g.top[b_mine], sbit = 8 * ((b_mine >> 1) & 3);
+    const int shift = mx_grad_shift<DT>((int)g.top[b_mine]), sbit = 8 * ((b_mine >> 1) & 3);
     const uint32_t a_code = base + P::DY + wb * 512 + wn * 16, a_scale = base + P::DY + P::CODES + (b_mine & 1) * 128 + wn * 4;
     const uint32_t a_wide = base + S * P::SLOT;
     uint32_t a_write[4], a_read[2];
@@ -340,7 +343,7 @@ __global__ __launch_bounds__(256) void mx_grad_any_kernel(const MxGrad g) {
                 const int b = c * 2 + kb;
                 t = b * 32 < g.K ? g.top[b] : 0;
             }
-            const float sc = mx_grad_scale(s, mx_grad_field<DT>() - (int)t);
+            const float sc = mx_grad_scale(s, mx_grad_shift<DT>((int)t));
 #pragma unroll
             for (int i = 0; i < 4; ++i) *(uint4v*)(wt + n * (BK * 2) + (((kb * 4 + i) ^ (n & 7)) << 4)) = mx_widen8<DT>(v[i], sc);
         }
@@ -372,7 +375,7 @@ __global__ __launch_bounds__(256) void mx_grad_any_kernel(const MxGrad g) {
     const long m = m0 + wm * 32 + (lane & 31);
     const int kcol = k0 + wk * 32, h = lane >> 5;
     if (kcol >= g.K || m >= g.M) return;
-    const int back = (int)g.top[kcol >> 5] - mx_grad_field<DT>();
+    const int back = -mx_grad_shift<DT>((int)g.top[kcol >> 5]);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int k = kcol + 8 * (i >> 2) + 4 * h + (i & 3);

@@ -625,3 +625,45 @@ def test_layer_norm_grad_far_mean(mq, C):
         within(f64(dx), want, err + half_step(np.abs(want) + err, BF16))
         assert not dw.any()
         within(f64(db), f64(dy).sum(0), (M + 70) * U * np.abs(f64(dy)).sum(0))
+
+
+# ----------------------------------------------------------------------------------------------- gradient: the ends of bfloat16's range
+
+@pytest.mark.parametrize("M,K,N", ((5, 64, 64), (45, 160, 72), (300, 352, 650), (9, 96, 71), (2, 1280, 9000)))
+def test_linear_grad_large_dy(mq, M, K, N):
+    """dY near the end of bfloat16's range, weights of ordinary size: results are finite, and so are the sums on the way."""
+    dy, w = rand((M, N), BF16, 94, 1.0, 0.0, False), rand((N, K), BF16, 95, 0.02, 0.0, False)
+    dy = (dy.float() * 2.0 ** 124).to(BF16)
+    dy[-1], dy[-1, 0] = 0.0, 3.3e38
+    check_grad(mq, dy, w)
+    dx = mq.mx_linear_grad(dy, mq.mx_quantize_weights(w))
+    assert torch.isfinite(dx).all()
+
+
+def test_linear_grad_far_scales(mq):
+    """Weights at both ends of bfloat16's range in one column of blocks, dY only on those at the lower one: they count for what they are."""
+    N, K = 64, 96
+    w = rand((N, K), BF16, 96, 1.0, 0.0, False)
+    w[:32] *= 2.0 ** 120
+    w[32:] *= 2.0 ** -110
+    dy = torch.zeros(6, N, dtype=BF16, device="cuda")
+    dy[:, 32:] = rand((6, 32), BF16, 97) * 2.0 ** 20
+    wq = mq.mx_quantize_weights(w)
+    v = omx.values(f64(w))
+    want, mag = omx.linear_grad(f64(dy), v)
+    acc = (N + 8) * 2 * U * mag
+    for rows in (1, 6):
+        within(f64(mq.mx_linear_grad(dy[:rows], wq)), want[:rows], acc[:rows] + half_step(np.abs(want[:rows]) + acc[:rows], BF16))
+
+
+@pytest.mark.parametrize("M,K,N", ((5, 64, 64), (9, 96, 71), (300, 352, 650)))
+def test_linear_grad_small_dy(mq, M, K, N):
+    """dY and results near the lower end, subnormal ones among them: a product of the matrix instructions below 2^-149 may go, a result is off by half a
+    step."""
+    w = rand((N, K), BF16, 98, 0.02)
+    for e in (-118, -122, -126):
+        dy = (rand((M, N), BF16, 99).float() * 2.0 ** e).to(BF16)
+        v = omx.values(f64(w))
+        want, mag = omx.linear_grad(f64(dy), v)
+        acc = (N + 8) * 2 * U * mag + (N + 8) * 2.0 ** -149
+        within(f64(mq.mx_linear_grad(dy, mq.mx_quantize_weights(w))), want, acc + half_step(np.abs(want) + acc, BF16))
