@@ -738,6 +738,7 @@ def alloc_search(sens_content, params_content, sens_quality, params_quality, bit
 # ------------------------------------------- microscaled 4-bit floats, layer norm, and their gradients
 #
 # Matrices are [rows, columns] with contiguous rows, which may lie apart but not over one another (so a broadcast one is made contiguous() first).
+# Results are no part of autograd's graph; gradients are calls of their own.
 
 
 _HALF = (None, torch.float16)  # mx_linear's default
@@ -768,6 +769,13 @@ def _matrix(t: torch.Tensor, rows=None, cols=None, dtype=None, device=None) -> t
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
     return t
+
+
+def _no_graph(what: str, *ts) -> None:
+    """Results carry no graph: what autograd would have to go through is refused rather than cut off from it."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in ts):
+        raise RuntimeError(f"{what} is no part of autograd's graph: call it under torch.no_grad(), or in the forward of a torch.autograd.Function, and "
+                           "mx_linear_grad and layer_norm_grad for the gradients")
 
 
 def _out(t: Optional[torch.Tensor], rows: int, cols: int, dtype, device) -> torch.Tensor:
@@ -897,6 +905,7 @@ def mx_linear(x: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[torc
             if r is not None:
                 return _done(r, "mq_mx_linear")
     lib = load()
+    _no_graph("mx_linear", None if packed else x, bias, residual)
     if packed:
         M, K, device = x.rows, x.K, x.data.device
         dtype = dtype or (out.dtype if out is not None else torch.float16)
@@ -934,6 +943,7 @@ def mx_linear_grad(dy: torch.Tensor, w: MxTensor, out: Optional[torch.Tensor] = 
         r = (_native or _load_native()).mx_linear_grad(dy, w.data, w.rows, w.K, w.top)
         if r is not None:
             return _done(r, "mq_mx_linear_grad")
+    _no_graph("mx_linear_grad", dy)
     M, N = _matrix(dy, cols=w.rows).shape
     dx = _out(out, M, w.K, dy.dtype, dy.device)
     ws = _mx_workspace(mx_linear_grad_workspace_bytes(M, N, w.K), dy.device, ws)
@@ -966,6 +976,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
         r = (_native or _load_native()).layer_norm(x, weight, bias, eps, want_stats, False)
         if r is not None:
             return _done(r, "mq_layer_norm")
+    _no_graph("layer_norm", x, weight, bias)
     M, N = _matrix(x).shape
     w, b, pt = _params(x, weight, bias)
     mean, rstd = _stats(x, want_stats)
@@ -982,6 +993,7 @@ def layer_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: 
     if r is not None:
         r = _done(r, "mq_layer_norm_mx")
         return (MxTensor(r[0], *x.shape), r[1], r[2]) if want_stats else MxTensor(r, *x.shape)
+    _no_graph("layer_norm_mx", x, weight, bias)
     M, N = _matrix(x).shape
     w, b, pt = _params(x, weight, bias)
     mean, rstd = _stats(x, want_stats)
@@ -1003,6 +1015,7 @@ def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Te
         r = (_native or _load_native()).layer_norm_grad(dy, x, weight, mean, rstd, residual)
         if r is not None:
             return _done(r, "mq_layer_norm_grad")
+    _no_graph("layer_norm_grad", dy)
     M, N = _matrix(x).shape
     _matrix(dy, M, N, x.dtype, x.device)
     if residual is not None:

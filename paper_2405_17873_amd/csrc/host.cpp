@@ -10,6 +10,7 @@
 // raises the errors.
 #include <ATen/ops/empty.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -338,6 +339,15 @@ bool mx_data(PyObject* o, int rows, int K, void*& p, const at::Tensor* beside = 
     p = t->data_ptr();
     return true;
 }
+// Whether autograd would have to go through a call with these operands (for the general way to refuse).
+bool in_graph(std::initializer_list<PyObject*> operands) {
+    if (!c10::GradMode::is_enabled()) return false;
+    for (PyObject* o : operands) {
+        const at::Tensor* t = o == Py_None ? nullptr : gpu_tensor(o);
+        if (t && t->requires_grad()) return true;
+    }
+    return false;
+}
 at::Tensor workspace(size_t bytes, at::Device device) { return empty({(int64_t)bytes}, at::kByte, device); }
 PyObject* pair_or_more(std::initializer_list<at::Tensor> list) {
     PyObject* t = PyTuple_New((Py_ssize_t)list.size());
@@ -402,7 +412,7 @@ PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int N, K;
         void *w, *bias;
         if (n != 6 || !plain_calls() || !matrix(a[0], x) || !small_int(a[2], N) || !small_int(a[3], K) || x.cols != K ||
-            !mx_data(a[1], N, K, w, x.t))
+            !mx_data(a[1], N, K, w, x.t) || in_graph({a[0], a[4], a[5]}))
             return general();
         const at::Device device = x.t->device();
         at::ScalarType type = x.t->scalar_type();
@@ -430,7 +440,7 @@ PyObject* mx_linear_codes(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int M, K, N, dtype;
         void *x, *w, *bias;
         if (n != 8 || !plain_calls() || !small_int(a[1], M) || !small_int(a[2], K) || !small_int(a[4], N) || !small_int(a[7], dtype) ||
-            (dtype != 0 && dtype != 1) || !mx_data(a[0], M, K, x) || !mx_data(a[3], N, K, w, gpu_tensor(a[0])))
+            (dtype != 0 && dtype != 1) || !mx_data(a[0], M, K, x) || !mx_data(a[3], N, K, w, gpu_tensor(a[0])) || in_graph({a[5], a[6]}))
             return general();
         const at::Device device = gpu_tensor(a[0])->device();
         const at::ScalarType want = dtype ? at::kBFloat16 : at::kHalf;
@@ -458,7 +468,8 @@ PyObject* mx_linear_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* w;
         const at::Tensor* top;
         if (n != 5 || !plain_calls() || !matrix(a[0], dy) || !small_int(a[2], N) || !small_int(a[3], K) || dy.cols != N || !mx_data(a[1], N, K, w, dy.t) ||
-            !(top = gpu_tensor(a[4])) || top->scalar_type() != at::kByte || !top->is_contiguous() || top->numel() != K / 32 || top->device() != dy.t->device())
+            !(top = gpu_tensor(a[4])) || top->scalar_type() != at::kByte || !top->is_contiguous() || top->numel() != K / 32 || top->device() != dy.t->device() ||
+            in_graph({a[0]}))
             return general();
         const void* tp = top->data_ptr();
         const at::Device device = dy.t->device();
@@ -500,7 +511,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int pt;
         bool stats, mx;
         if (n != 6 || !plain_calls() || !matrix(a[0], x) || !norm_params(a[1], a[2], x, w, b, pt) || !PyFloat_CheckExact(a[3]) || !flag(a[4], stats) ||
-            !flag(a[5], mx) || (mx && x.cols % 32 != 0))
+            !flag(a[5], mx) || (mx && x.cols % 32 != 0) || in_graph({a[0], a[1], a[2]}))
             return general();
         const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
         const at::Device device = x.t->device();
@@ -532,7 +543,7 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (n != 6 || !plain_calls() || !matrix(a[1], x) || !matrix(a[0], dy) || dy.rows != x.rows || dy.cols != x.cols || dy.dtype != x.dtype ||
             !norm_params(a[2], Py_None, x, w, b, pt) || !vector(a[3], x.rows, x.t->device(), mean, &tm) ||
             !vector(a[4], x.rows, x.t->device(), rstd, &tr) || !mean || !rstd || tm != at::kFloat || tr != at::kFloat ||
-            dy.t->device() != x.t->device() || !optional_matrix(a[5], x.rows, x.cols, x.dtype, x.t->device(), res))
+            dy.t->device() != x.t->device() || !optional_matrix(a[5], x.rows, x.cols, x.dtype, x.t->device(), res) || in_graph({a[0]}))
             return general();
         const at::Device device = x.t->device();
         at::Tensor dx, dw, db, ws;

@@ -667,3 +667,35 @@ def test_linear_grad_small_dy(mq, M, K, N):
         want, mag = omx.linear_grad(f64(dy), v)
         acc = (N + 8) * 2 * U * mag + (N + 8) * 2.0 ** -149
         within(f64(mq.mx_linear_grad(dy, mq.mx_quantize_weights(w))), want, acc + half_step(np.abs(want) + acc, BF16))
+
+
+def test_graphs_are_refused(mq):
+    """Operands that require a gradient: refused where autograd is on, the same bits as without where it is off, and in a torch.autograd.Function."""
+    M, K, N = 40, 64, 96
+    x, w, b, r = rand((M, K), F16, 100), mq.mx_quantize_weights(rand((N, K), F16, 101, 0.05)), rand((N,), F16, 102), rand((M, N), F16, 103)
+    gain, shift = params(K, "f32", F16, 104)
+    _, mean, rstd = mq.layer_norm(x, want_stats=True)
+    xq = mq.mx_quantize(x)
+    g = lambda t: t.clone().requires_grad_()
+    calls = ((lambda x: mq.mx_linear(x, w, b), x), (lambda b: mq.mx_linear(x, w, b), b), (lambda r: mq.mx_linear(x, w, b, residual=r), r),
+             (lambda b: mq.mx_linear(xq, w, b), b), (lambda r: mq.mx_linear(xq, w, b, residual=r), r), (lambda x: mq.layer_norm(x, gain, shift), x),
+             (lambda p: mq.layer_norm(x, p, shift), gain), (lambda p: mq.layer_norm(x, gain, p), shift), (lambda p: mq.layer_norm_mx(x, p, shift).data, gain),
+             (lambda d: mq.mx_linear_grad(d, w), r), (lambda d: mq.layer_norm_grad(d, x, gain, mean, rstd)[0], x))
+    for call, t in calls:
+        with pytest.raises(RuntimeError, match="graph"):
+            call(g(t))
+        with torch.no_grad():
+            assert torch.equal(call(g(t)), call(t))
+
+    class Linear(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            return mq.mx_linear(x, w, b)
+
+        @staticmethod
+        def backward(ctx, dy):
+            return mq.mx_linear_grad(dy, w)
+
+    leaf = g(x)
+    Linear.apply(leaf).backward(r)
+    assert torch.equal(leaf.grad, mq.mx_linear_grad(r, w))

@@ -251,3 +251,21 @@ int main() {
         if name.startswith("mx_"):
             for line in open(os.path.join(csrc, name)):
                 assert not re.search(r"static\s+const\s+hipError_t", line), f"{name} keeps one device's answer for all: {line}"
+
+
+def test_graphs_are_refused(lib):
+    """A result that autograd would have to know of is refused, with the operands as they come; without autograd the same operands pass that check."""
+    import torch
+
+    import paper_2405_17873_amd as mq
+    x, p = torch.zeros(4, 64, dtype=torch.float16), torch.zeros(64)
+    w = mq.MxTensor(torch.zeros(mq.mx_bytes(64, 64), dtype=torch.uint8), 64, 64, torch.zeros(2, dtype=torch.uint8))
+    gx, gp, gb = (t.clone().requires_grad_() for t in (x, p, p.half()))
+    calls = (lambda: mq.mx_linear(gx, w), lambda: mq.mx_linear(x, w, gb), lambda: mq.mx_linear(x, w, residual=gx), lambda: mq.mx_linear(w, w, gb),
+             lambda: mq.layer_norm(gx), lambda: mq.layer_norm(x, gp, p), lambda: mq.layer_norm(x, p, gp), lambda: mq.layer_norm_mx(gx), lambda: mq.layer_norm_mx(x, gp),
+             lambda: mq.mx_linear_grad(gx, w), lambda: mq.layer_norm_grad(gx, x, p, p, p))
+    for call in calls:
+        with pytest.raises(RuntimeError, match="graph"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError):  # (on the host)
+            call()
