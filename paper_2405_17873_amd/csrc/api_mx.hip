@@ -149,7 +149,7 @@ int mq_layer_norm(const void* x, int M, int C, long ldx, const void* weight, con
                   float* mean, float* rstd, void* stream) {
     int rc;
     if ((rc = check_norm(x, M, C, ldx, weight, bias, param_dtype, dtype)) || (rc = check_matrix(y, M, ldy, C))) return rc;
-    if (!(eps >= 0.0f)) return MQ_ERR_BAD_ARG;
+    if (!(eps >= 0.0f) || !aligned(mean, 4) || !aligned(rstd, 4)) return MQ_ERR_BAD_ARG;
     if (M == 0) return MQ_OK;
     NormArgs a = {};
     a.x = (const uint16_t*)x, a.ldx = ldx, a.M = M, a.C = C, a.weight = weight, a.bias = bias, a.param_dtype = param_dtype, a.eps = eps;
@@ -161,7 +161,7 @@ int mq_layer_norm_mx(const void* x, int M, int C, long ldx, const void* weight, 
                      float* mean, float* rstd, void* stream) {
     int rc;
     if ((rc = check_norm(x, M, C, ldx, weight, bias, param_dtype, dtype)) || (rc = check_mx(mx, M, C))) return rc;
-    if (!(eps >= 0.0f)) return MQ_ERR_BAD_ARG;
+    if (!(eps >= 0.0f) || !aligned(mean, 4) || !aligned(rstd, 4)) return MQ_ERR_BAD_ARG;
     if (M == 0) return MQ_OK;
     NormArgs a = {};
     a.x = (const uint16_t*)x, a.ldx = ldx, a.M = M, a.C = C, a.weight = weight, a.bias = bias, a.param_dtype = param_dtype, a.eps = eps;
@@ -179,6 +179,7 @@ int mq_layer_norm_grad(const void* dy, long lddy, const void* x, long ldx, int M
         return rc;
     if (residual && (rc = check_matrix(residual, M, ldr, C))) return rc;
     if (M > 0 && (!mean || !rstd || !ws || !aligned(ws, 256))) return MQ_ERR_BAD_ARG;
+    if (!aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dweight, 4) || !aligned(dbias, 4)) return MQ_ERR_BAD_ARG;
     if (ws_bytes < mq_layer_norm_grad_workspace_bytes(M, C)) return MQ_ERR_WORKSPACE_TOO_SMALL;
     NormArgs a = {};
     a.x = (const uint16_t*)x, a.ldx = ldx, a.M = M, a.C = C, a.weight = weight, a.param_dtype = param_dtype, a.dtype = dtype;

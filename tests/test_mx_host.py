@@ -269,3 +269,16 @@ def test_graphs_are_refused(lib):
             call()
         with torch.no_grad(), pytest.raises(ValueError):  # (on the host)
             call()
+
+
+def test_float_pointers_are_looked_at(lib):
+    """Statistics and sums are float32: addresses off four bytes are refused, and so are 16-bit operands off two."""
+    buf = (C.c_uint8 * 4096)()
+    p = C.c_void_p((C.addressof(buf) + 255) // 256 * 256)  # every call below fails before it is used
+    half, null, st, L, f = C.c_void_p(p.value + 2), C.c_void_p(0), C.c_void_p(0), C.c_long, C.c_float
+    ln = lambda mean=null, rstd=null: lib.mq_layer_norm(p, 4, 64, L(64), null, null, 2, f(1e-5), p, L(64), 0, mean, rstd, st)
+    lm = lambda mean=null, rstd=null: lib.mq_layer_norm_mx(p, 4, 64, L(64), null, null, 2, f(1e-5), p, 0, mean, rstd, st)
+    assert ln(mean=half) == -1 and ln(rstd=half) == -1 and lm(mean=half) == -1 and lm(rstd=half) == -1
+    lg = lambda mean=p, rstd=p, dw=p, db=p: lib.mq_layer_norm_grad(p, L(64), p, L(64), 4, 64, null, 2, mean, rstd, null, L(0), p, L(64), 0, dw, db, p,
+                                                                   C.c_size_t(1 << 20), st)
+    assert lg(mean=half) == -1 and lg(rstd=half) == -1 and lg(dw=half) == -1 and lg(db=half) == -1
