@@ -925,7 +925,7 @@ def mx_linear(x: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[torc
         _check(lib.mq_mx_linear_codes(_mx_data(x, device), M, K, *args, _stream()), "mq_mx_linear_codes")
     else:
         # (a few rows do without, unless the output lies over them)
-        ws = _mx_workspace(mx_linear_workspace_bytes(M, w.rows, K) if out is None else mx_bytes(M, K), device, ws)
+        ws = _mx_workspace(mx_linear_workspace_bytes(M, w.rows, K) or (0 if out is None else mx_bytes(M, K)), device, ws)
         _check(lib.mq_mx_linear(_ptr(x), M, K, _ld(x), *args, _ptr(ws), _bytes_of(ws), _stream()), "mq_mx_linear")
     return y
 

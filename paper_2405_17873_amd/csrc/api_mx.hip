@@ -15,8 +15,9 @@ static int check_matrix(const void* p, int rows, long ld, int cols) {
     if (rows > 0 && (!p || !aligned(p, 2))) return MQ_ERR_BAD_ARG;
     return MQ_OK;
 }
+static bool mx_size_ok(int rows, int K) { return rows >= 0 && rows <= (1 << 28) && K > 0 && K % 32 == 0 && K <= (1 << 21); }
 static int check_mx(const void* p, int rows, int K) {
-    if (rows < 0 || K <= 0 || K % 32 != 0 || K > (1 << 21) || rows > (1 << 28)) return MQ_ERR_BAD_SHAPE;
+    if (!mx_size_ok(rows, K)) return MQ_ERR_BAD_SHAPE;
     if (rows > 0 && (!p || !aligned(p, 256))) return MQ_ERR_BAD_ARG;
     return MQ_OK;
 }
@@ -65,7 +66,7 @@ using namespace mq;
 
 extern "C" {
 
-size_t mq_mx_bytes(int rows, int K) { return rows < 0 || K <= 0 || K % 32 != 0 ? 0 : mx_bytes(rows, K); }
+size_t mq_mx_bytes(int rows, int K) { return mx_size_ok(rows, K) ? mx_bytes(rows, K) : 0; }
 
 int mq_mx_quantize(const void* x, int M, int K, long ldx, int dtype, void* mx, void* stream) {
     if (!type_ok(dtype)) return MQ_ERR_BAD_ARG;

@@ -282,3 +282,10 @@ def test_float_pointers_are_looked_at(lib):
     lg = lambda mean=p, rstd=p, dw=p, db=p: lib.mq_layer_norm_grad(p, L(64), p, L(64), 4, 64, null, 2, mean, rstd, null, L(0), p, L(64), 0, dw, db, p,
                                                                    C.c_size_t(1 << 20), st)
     assert lg(mean=half) == -1 and lg(rstd=half) == -1 and lg(dw=half) == -1 and lg(db=half) == -1
+
+
+def test_sizes_past_the_limits(lib):
+    """A size that no call takes has no bytes."""
+    import paper_2405_17873_amd as mq
+    assert mq.mx_bytes(4, 1 << 21) > 0 and mq.mx_bytes(4, (1 << 21) + 32) == 0
+    assert mq.mx_bytes(1 << 28, 32) > 0 and mq.mx_bytes((1 << 28) + 1, 32) == 0
