@@ -15,6 +15,18 @@ static int check_matrix(const void* p, int rows, long ld, int cols) {
     if (rows > 0 && (!p || !aligned(p, 2))) return MQ_ERR_BAD_ARG;
     return MQ_OK;
 }
+// Whether two matrices of M rows share no value: one lies behind the other, or the rows of one between those of the other.
+static bool apart(const void* a, long lda, int ca, const void* b, long ldb, int cb, int M) {
+    const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
+    if (q >= p + ((size_t)(M - 1) * lda + ca) * 2 || p >= q + ((size_t)(M - 1) * ldb + cb) * 2) return true;
+    if (M == 1 || lda != ldb) return false;
+    const size_t row = (size_t)lda * 2, behind = q >= p ? (q - p) % row : (row - (p - q) % row) % row;  // of b's first value in a row of a's
+    return behind >= (size_t)ca * 2 && behind + (size_t)cb * 2 <= row;
+}
+// An output that is written while others still read an operand: the operand itself (a thread reads its values before it writes them) or apart from it.
+static bool itself_or_apart(const void* out, long ldo, const void* in, long ldi, int cols, int M) {
+    return !in || (out == in && (ldo == ldi || M == 1)) || apart(out, ldo, cols, in, ldi, cols, M);
+}
 static bool mx_size_ok(int rows, int K) { return rows >= 0 && rows <= (1 << 28) && K > 0 && K % 32 == 0 && K <= (1 << 21); }
 static int check_mx(const void* p, int rows, int K) {
     if (!mx_size_ok(rows, K)) return MQ_ERR_BAD_SHAPE;
@@ -112,10 +124,10 @@ int mq_mx_linear(const void* x, int M, int K, long ldx, const void* w, int N, co
     int rc;
     if ((rc = check_product(M, N, K, w, bias, y, ldy, dtype, residual, ldr)) || (rc = check_matrix(x, M, ldx, K))) return rc;
     if (M == 0) return MQ_OK;
+    if (!itself_or_apart(y, ldy, residual, ldr, N, M)) return MQ_ERR_BAD_ARG;
     MxGemm g = product(M, K, w, N, bias, y, ldy, dtype, residual, ldr);
     // (one launch reads activations while others of its workgroups store results)
-    const bool apart = (uintptr_t)y >= (uintptr_t)x + ((size_t)(M - 1) * ldx + K) * 2 || (uintptr_t)x >= (uintptr_t)y + ((size_t)(M - 1) * ldy + N) * 2;
-    if (apart && mx_rows_quantizes(M, N, K)) return launch_mx_rows(g, x, ldx, (hipStream_t)stream);
+    if (mx_rows_quantizes(M, N, K) && apart(x, ldx, K, y, ldy, N, M)) return launch_mx_rows(g, x, ldx, (hipStream_t)stream);
     if (!ws || !aligned(ws, 256)) return MQ_ERR_BAD_ARG;
     if (ws_bytes < up256(mx_bytes(M, K))) return MQ_ERR_WORKSPACE_TOO_SMALL;
     if ((rc = launch_mx_quantize(x, M, K, ldx, dtype, ws, (hipStream_t)stream))) return rc;
@@ -127,6 +139,7 @@ int mq_mx_linear_codes(const void* a, int M, int K, const void* w, int N, const 
     int rc;
     if ((rc = check_product(M, N, K, w, bias, y, ldy, dtype, residual, ldr)) || (rc = check_mx(a, M, K))) return rc;
     if (M == 0) return MQ_OK;
+    if (!itself_or_apart(y, ldy, residual, ldr, N, M)) return MQ_ERR_BAD_ARG;
     MxGemm g = product(M, K, w, N, bias, y, ldy, dtype, residual, ldr);
     return run(g, a, (hipStream_t)stream);
 }
@@ -143,6 +156,7 @@ int mq_mx_linear_grad(const void* dy, int M, int N, long lddy, const void* w, co
     const size_t need = mq_mx_linear_grad_workspace_bytes(M, N, K);
     if (need > 0 && (!ws || !aligned(ws, 256))) return MQ_ERR_BAD_ARG;
     if (ws_bytes < need) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    if (!apart(dx, lddx, K, dy, lddy, N, M)) return MQ_ERR_BAD_ARG;
     return launch_mx_grad(dy, M, N, lddy, w, top, K, dx, lddx, dtype, ws, (hipStream_t)stream);
 }
 
@@ -152,6 +166,7 @@ int mq_layer_norm(const void* x, int M, int C, long ldx, const void* weight, con
     if ((rc = check_norm(x, M, C, ldx, weight, bias, param_dtype, dtype)) || (rc = check_matrix(y, M, ldy, C))) return rc;
     if (!(eps >= 0.0f) || !aligned(mean, 4) || !aligned(rstd, 4)) return MQ_ERR_BAD_ARG;
     if (M == 0) return MQ_OK;
+    if (!itself_or_apart(y, ldy, x, ldx, C, M)) return MQ_ERR_BAD_ARG;
     NormArgs a = {};
     a.x = (const uint16_t*)x, a.ldx = ldx, a.M = M, a.C = C, a.weight = weight, a.bias = bias, a.param_dtype = param_dtype, a.eps = eps;
     a.dtype = dtype, a.mean = mean, a.rstd = rstd, a.y = (uint16_t*)y, a.ldy = ldy;
@@ -182,6 +197,8 @@ int mq_layer_norm_grad(const void* dy, long lddy, const void* x, long ldx, int M
     if (M > 0 && (!mean || !rstd || !ws || !aligned(ws, 256))) return MQ_ERR_BAD_ARG;
     if (!aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dweight, 4) || !aligned(dbias, 4)) return MQ_ERR_BAD_ARG;
     if (ws_bytes < mq_layer_norm_grad_workspace_bytes(M, C)) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    if (M > 0 && !(itself_or_apart(dx, lddx, dy, lddy, C, M) && itself_or_apart(dx, lddx, x, ldx, C, M) && itself_or_apart(dx, lddx, residual, ldr, C, M)))
+        return MQ_ERR_BAD_ARG;
     NormArgs a = {};
     a.x = (const uint16_t*)x, a.ldx = ldx, a.M = M, a.C = C, a.weight = weight, a.param_dtype = param_dtype, a.dtype = dtype;
     a.mean = (float*)mean, a.rstd = (float*)rstd, a.dy = (const uint16_t*)dy, a.lddy = lddy, a.res = (const uint16_t*)residual, a.ldr = ldr;

@@ -699,3 +699,31 @@ def test_graphs_are_refused(mq):
     leaf = g(x)
     Linear.apply(leaf).backward(r)
     assert torch.equal(leaf.grad, mq.mx_linear_grad(r, w))
+
+
+def test_outputs_over_operands(mq):
+    """Outputs whose rows lie between those of an operand are as any other; ones over an operand are refused."""
+    M, K, N = 37, 64, 64
+    w = mq.mx_quantize_weights(rand((N, K), F16, 110, 0.05))
+    x, r = rand((M, K), F16, 111), rand((M, N), F16, 112)
+    _, mean, rstd = mq.layer_norm(x, want_stats=True)
+    both = lambda t: (lambda b: (b[:, :64], b[:, 64:]))(torch.cat([t, torch.zeros_like(t)], 1))
+    for rows in (1, 5, M):
+        a, out = both(r[:rows])
+        assert torch.equal(mq.mx_linear_grad(a, w, out=out), mq.mx_linear_grad(r[:rows], w))
+        for t in (x[:rows], mq.mx_quantize(x[:rows])):
+            a, out = both(r[:rows])
+            assert torch.equal(mq.mx_linear(t, w, residual=a, out=out), mq.mx_linear(t, w, residual=r[:rows]))
+        a, out = both(x[:rows])
+        assert torch.equal(mq.mx_linear(a, w, out=out), mq.mx_linear(x[:rows], w))
+        a, out = both(x[:rows])
+        assert torch.equal(mq.layer_norm(a, out=out), mq.layer_norm(x[:rows]))
+        a, out = both(r[:rows])
+        for got, want in zip(mq.layer_norm_grad(a, x[:rows], None, mean[:rows], rstd[:rows], out=out), mq.layer_norm_grad(r[:rows], x[:rows], None, mean[:rows], rstd[:rows])):
+            assert torch.equal(got, want)
+    b = torch.cat([x, x], 0)
+    for call in (lambda: mq.mx_linear_grad(b[:M], w, out=b[:M]), lambda: mq.mx_linear_grad(b[:M], w, out=b[1:M + 1]), lambda: mq.mx_linear(x, w, residual=b[:M], out=b[1:M + 1]),
+                 lambda: mq.mx_linear(mq.mx_quantize(x), w, residual=b[1:M + 1], out=b[:M]), lambda: mq.layer_norm(b[:M], out=b[3:M + 3]),
+                 lambda: mq.layer_norm_grad(b[:M], x, None, mean, rstd, out=b[1:M + 1])):
+        with pytest.raises(mq.MixdqError):
+            call()

@@ -289,3 +289,26 @@ def test_sizes_past_the_limits(lib):
     import paper_2405_17873_amd as mq
     assert mq.mx_bytes(4, 1 << 21) > 0 and mq.mx_bytes(4, (1 << 21) + 32) == 0
     assert mq.mx_bytes(1 << 28, 32) > 0 and mq.mx_bytes((1 << 28) + 1, 32) == 0
+
+
+def test_outputs_over_operands_are_refused(lib):
+    """An output that lies over an operand without being that operand, row for row."""
+    buf = (C.c_uint8 * 65536)()
+    p = C.c_void_p((C.addressof(buf) + 255) // 256 * 256)  # every call below fails before it is used
+    null, st, L, f = C.c_void_p(0), C.c_void_p(0), C.c_long, C.c_float
+    at = lambda values: C.c_void_p(p.value + 2 * values)
+    far = C.c_void_p(p.value + (1 << 30))
+    gr = lambda dx=p, lddx=64, K=64, N=64, ld=64: lib.mq_mx_linear_grad(p, 4, N, L(ld), far, far, K, dx, L(lddx), 0, null, C.c_size_t(0), st)
+    assert gr() == -1 and gr(dx=at(255)) == -1 and gr(dx=at(64)) == -1 and gr(dx=at(63), lddx=128, ld=128) == -1 and gr(dx=at(-255)) == -1
+    assert gr(dx=at(64), lddx=128, ld=127) == -1  # rows of another distance: taken as one over the other
+    lin = lambda r, ldr, y=p, ldy=64, M=40, codes=0: (lib.mq_mx_linear_codes(far, M, 64, far, 64, null, y, L(ldy), 0, r, L(ldr), st) if codes else lib.mq_mx_linear(
+        far, M, 64, L(64), far, 64, null, y, L(ldy), 0, r, L(ldr), far, C.c_size_t(1 << 20), st))
+    for codes in (0, 1):
+        for M in (4, 40, 200):
+            assert lin(at(64), 64, M=M, codes=codes) == -1 and lin(at(1), 64, M=M, codes=codes) == -1 and lin(p, 128, M=M, codes=codes) == -1
+            assert lin(at(63), 128, ldy=128, M=M, codes=codes) == -1
+    ln = lambda y, ldy: lib.mq_layer_norm(p, 4, 64, L(64), null, null, 2, f(1e-5), y, L(ldy), 0, null, null, st)
+    assert ln(at(64), 64) == -1 and ln(at(1), 64) == -1 and ln(p, 128) == -1 and ln(at(-64), 64) == -1
+    lg = lambda dx=far, lddx=64, dy=at(4096), x=at(8192), r=null: lib.mq_layer_norm_grad(
+        dy, L(64), x, L(64), 4, 64, null, 2, p, p, r, L(64), dx, L(lddx), 0, p, p, p, C.c_size_t(1 << 20), st)
+    assert lg(dx=at(4096 + 64)) == -1 and lg(dx=at(8192 - 64)) == -1 and lg(dx=at(100), r=at(99)) == -1 and lg(dx=at(4096), lddx=65) == -1
