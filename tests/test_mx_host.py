@@ -312,3 +312,15 @@ def test_outputs_over_operands_are_refused(lib):
     lg = lambda dx=far, lddx=64, dy=at(4096), x=at(8192), r=null: lib.mq_layer_norm_grad(
         dy, L(64), x, L(64), 4, 64, null, 2, p, p, r, L(64), dx, L(lddx), 0, p, p, p, C.c_size_t(1 << 20), st)
     assert lg(dx=at(4096 + 64)) == -1 and lg(dx=at(8192 - 64)) == -1 and lg(dx=at(100), r=at(99)) == -1 and lg(dx=at(4096), lddx=65) == -1
+
+
+def test_values_are_their_own():
+    """Quantised values quantise to themselves: a block's largest, 4 to 8 units before, is 4 or 6 units after, and so has the same scale."""
+    rng = np.random.default_rng(7)
+    for std in (1.0, 1e-3, 1e30, 2.0 ** -126, 2.0 ** -130):
+        x = rng.normal(size=(40, 96)) * std
+        x[rng.random(x.shape) < 0.05] *= 9.0
+        x[3], x[4, 32:64], x[5, :32] = 0.0, std * 7.9, std * 6.0
+        v = omx.values(x)
+        assert np.abs(v).max() > 0 and np.array_equal(omx.values(v), v)
+        assert np.array_equal(omx.scale_bytes(v), omx.scale_bytes(x))
