@@ -727,3 +727,46 @@ def test_outputs_over_operands(mq):
                  lambda: mq.layer_norm_grad(b[:M], x, None, mean, rstd, out=b[1:M + 1])):
         with pytest.raises(mq.MixdqError):
             call()
+
+
+# --------------------------------------------------------------------------------------------------- many rows, many tiles
+
+# Rows of 640 columns are walked 16 at a time by each of 256 workgroups, 1280 8, 4096 one, 33 columns 32: a walk of two or three turns, the last one cut off.
+# (637 and 2049 columns, and rows that start anywhere, take the form that loads value by value.)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,C,per,kind", ((9001, 640, 16, "f32"), (4500, 1280, 8, "16"), (700, 4096, 1, "16"), (2100, 2560, 4, "f32"), (16500, 320, 32, "16"),
+                                          (5001, 637, 16, "f32"), (1100, 2049, 4, "16"), (8300, 33, 32, "none")))
+def test_layer_norm_grad_many_rows(mq, M, C, per, kind, dtype):
+    assert M > 256 * per  # a second turn
+    x, dy, res = rand((M, C), dtype, M + C, 1.0, 0.5), rand((M, C), dtype, M + C + 1), rand((M, C), dtype, 120)
+    w, b = params(C, kind, dtype, 121)
+    _, mean, rstd = mq.layer_norm(x, w, b, 1e-5, want_stats=True)
+    W, _ = p64(w, b, C)
+    X, DY, R, mu, r = f64(x), f64(dy), f64(res), f64(mean)[:, None], f64(rstd)[:, None]
+    xh, g = (X - mu) * r, DY * W
+    exh = 3 * U * (np.abs(X) + np.abs(mu)) * r
+    n = depth(C)
+    m1, m2 = np.abs(g).mean(-1, keepdims=True), (np.abs(g) * (np.abs(xh) + exh)).mean(-1, keepdims=True)
+    e1, e2 = (n + 4) * U * m1, (n + 6) * U * m2 + (np.abs(g) * exh).mean(-1, keepdims=True)
+    # additions of a column's sum: the turns of a walk, the rows of a workgroup that lie side by side, up to 8 workgroups in a run, 32 runs
+    adds = -(-M // (256 * per)) + per + 8 + 32
+    for res_, R_ in ((res, R), (None, None)):
+        wantx, wantw, wantb = omx.norm_grad(DY, X, W, mu, r, R_)
+        err = r * (6 * U * (np.abs(g) + m1 + np.abs(xh) * m2) + e1 + np.abs(xh) * e2 + exh * m2) + (0 if R_ is None else 2 * U * np.abs(R_)) + 2 * U * np.abs(wantx)
+
+        def check(got):
+            within(f64(got[0]), wantx, err + half_step(np.abs(wantx) + err, dtype), "dx")
+            within(f64(got[1]), wantw, ((adds + 2) * U * np.abs(DY * xh) + np.abs(DY) * exh).sum(0) + 2.0 ** -126, "dweight")
+            within(f64(got[2]), wantb, adds * U * np.abs(DY).sum(0) + 2.0 ** -126, "dbias")
+
+        got = mq.layer_norm_grad(dy, x, w, mean, rstd, residual=res_)
+        check(got)
+        # dX over dY, over the residual: the same bits; in rows that start anywhere: another form, the same bounds
+        d = dy.clone()
+        assert all(torch.equal(a, c) for a, c in zip(mq.layer_norm_grad(d, x, w, mean, rstd, residual=res_, out=d), got))
+        if res_ is not None:
+            o = res.clone()
+            assert all(torch.equal(a, c) for a, c in zip(mq.layer_norm_grad(dy, x, w, mean, rstd, residual=o, out=o), got))
+        o = spread(torch.zeros_like(x), 5, 3)
+        check(mq.layer_norm_grad(spread(dy, 3, 1), spread(x, 1, 0), w, mean, rstd, residual=None if res_ is None else spread(res, 5, 7), out=o))
+        assert int(torch.isnan(o._base).sum()) == o._base.numel() - M * C
