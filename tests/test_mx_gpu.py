@@ -770,3 +770,49 @@ def test_layer_norm_grad_many_rows(mq, M, C, per, kind, dtype):
         o = spread(torch.zeros_like(x), 5, 3)
         check(mq.layer_norm_grad(spread(dy, 3, 1), spread(x, 1, 0), w, mean, rstd, residual=None if res_ is None else spread(res, 5, 7), out=o))
         assert int(torch.isnan(o._base).sum()) == o._base.numel() - M * C
+
+
+def exact_on_device(t):
+    import paper_2405_17873_amd as m
+    return m.mx_dequantize(t, BF16).double()  # (exact: two significant bits)
+
+
+# Tiles of 128 rows x 128 columns in a whole round of 256 workgroups and a last round cut in two and four (6618, 6650, 4096), cut alone (4215) and whole (5557);
+# of 64 rows in a whole round and four parts (5651, 5700), whole (4366); of 32 (1000, 20 in six parts).  Rows copied first where N is no multiple of eight.
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K,N", ((6618, 544, 2066), (6650, 544, 2072), (4096, 1280, 10240), (4215, 32, 5107), (5557, 288, 40), (5651, 288, 4803), (5700, 288, 4808),
+                                   (4366, 160, 32), (1000, 352, 640), (20, 5120, 20480)))
+def test_linear_grad_tiles(mq, M, K, N, dtype):
+    """Every element, against a float64 product."""
+    dy, w = rand((M, N), dtype, M + N), rand((N, K), dtype, K, 0.02)
+    wq = mq.mx_quantize_weights(w)
+    v = exact_on_device(wq)
+    d = dy.double()
+    want, acc = d @ v, (d.abs() @ v.abs()) * ((N + 8) * 2 * U)
+    top = v.abs().view(N, -1, 32).amax((0, 2)).repeat_interleave(32)
+    acc += d.abs().sum(1, keepdim=True) * top * 2.0 ** -36
+    bound = acc + torch.finfo(dtype).eps / 2 * (want.abs() + acc) + (2.0 ** -25 if dtype == F16 else 2.0 ** -133)
+    for out in (None, spread(torch.zeros(M, K, dtype=dtype, device="cuda"), 8, 8)):
+        dx = mq.mx_linear_grad(dy, wq, out=out)
+        assert int(((dx.double() - want).abs() > bound).sum()) == 0
+        if out is not None:
+            assert int(torch.isnan(out._base).sum()) == out._base.numel() - M * K
+
+
+@pytest.mark.parametrize("M,K,N", ((8200, 704, 4104), (33000, 320, 1032), (2400, 640, 1944), (1190, 992, 4200), (6000, 1280, 1600), (2100, 1280, 3848)))
+def test_linear_tiles_bfloat16(mq, M, K, N):
+    """The tiles of test_linear_tiles in the other type: 256 x 256, 128 x 160 and several of 128 x 128 to a workgroup, cut off on both sides; every element."""
+    x, w, b, r = rand((M, K), BF16, 11), rand((N, K), BF16, 12, 0.02), rand((N,), BF16, 13, 0.1), rand((M, N), BF16, 14)
+    wq, xq = mq.mx_quantize_weights(w), mq.mx_quantize(x)
+    xv, wv = exact_on_device(xq), exact_on_device(wq)
+    want, mag = xv @ wv.T + b.double(), xv.abs() @ wv.abs().T + b.double().abs()
+    for res in (None, r):
+        if res is not None:
+            want, mag = want + res.double(), mag + res.double().abs()
+        acc = (K + 4) * 2 * U * mag
+        bound = acc + torch.finfo(BF16).eps / 2 * (want.abs() + acc) + 2.0 ** -133
+        for t in (xq, x):
+            y = mq.mx_linear(t, wq, b, residual=res, dtype=BF16)
+            assert int(((y.double() - want).abs() > bound).sum()) == 0
+    o = r.clone()
+    assert torch.equal(mq.mx_linear(xq, wq, b, residual=o, dtype=BF16, out=o), y)
