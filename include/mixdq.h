@@ -405,7 +405,8 @@ int mq_bos_aware_kv_proj(const void* ctx, int B, int T, int K, const void* packe
  * (256-byte aligned, mq_mx_bytes); mq_mx_pack and mq_mx_unpack convert from and to rows of codes and scales.
  *
  * In this section row strides are `long` and any value of at least a row; 16-bit matrices need no alignment beyond their type's.  (N, K and C that
- * are multiples of eight are faster, in the gradients also rows that start on 16-byte boundaries; a long N that is not takes room for a copy of dY.)  A call with M = 0 rows is MQ_OK and writes nothing but zero sums (mq_layer_norm_grad).
+ * are multiples of eight are faster, in the gradients also rows that start on 16-byte boundaries; a long N that is not takes room for a copy of dY.)  A call
+ * with M = 0 rows is MQ_OK and writes nothing but zero sums (mq_layer_norm_grad).
  * An output may be an operand only where that is said, and then with its row stride; one that shares values with an operand in another way is refused.
  * Errors beside those named: MQ_ERR_BAD_ARG (null or misaligned pointer, unknown dtype, negative or NaN eps, such an output), MQ_ERR_BAD_SHAPE (M < 0, K or C <= 0, K
  * not a multiple of 32, a stride below the row, K > 2^21, N > 2^22, C > 16384, more than 2^28 rows of a microscaled matrix), MQ_ERR_HIP.

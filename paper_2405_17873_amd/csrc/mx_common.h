@@ -21,7 +21,6 @@ struct MxView {  // host and device: where the parts of a matrix of `rows` x K l
     const uint8_t* codes;
     const uint8_t* scales;
     int groups, kc, kq;
-    __host__ __device__ static long group_bytes(int kc) { return (long)kc * 1024; }
 };
 inline size_t mx_bytes(long rows, long K) {
     const size_t G = (size_t)(rows + 31) / 32, KC = (size_t)(K + 63) / 64, KQ = (KC + 3) / 4;

@@ -101,10 +101,10 @@ struct MxPlan {
 // 128 k.  The fragments of the next 64 k are read while the MFMAs of this one run, and the loads of a later step are laid out between them one by one.
 // In the middle of a step every wave has read all of its slot; there all of them wait for the next step's.  A workgroup has several tiles, and the steps
 // of one follow those of another without a pause: while results are stored the next tile's first steps are on their way.
-// Bound by LDS and the MFMAs together where K is long: a step of a 256 x 256 tile writes 37 KB and reads 96, 1040 cycles of LDS, for 1024 of MFMAs; of
-// 8192 x 8192 x 8192 (255 us) the MFMAs take 60 %, and random operands half as long again as zeros, from the power they draw.  Four waves of 128 x 128 each
-// would read 64 KB, but spill and wait for themselves (338 us).  Where K is short, by the results: 16384 x 640 x 5120 writes 168 MB in 56 to 60 us, 42
-// without its stores; keeping results in registers and storing them between the MFMAs of the next tile (128 x 128 tiles) changed nothing, 64 us.
+// Bound by power where K is long: in 8192 x 8192 x 8192 (250 us) MFMAs run in 60 % of the cycles and LDS reads in 28 %, the clock falls to 1.7 GHz, and
+// random operands take half as long again as zeros.  Four waves of 128 x 128 each would read two thirds as much from LDS, but spill and wait for themselves
+// (338 us).  Where K is short, by the results: 16384 x 640 x 5120 writes 168 MB in 49 (traced) to 56 us, 42 without its stores; keeping results in registers
+// and storing them between the MFMAs of the next tile (128 x 128 tiles) changed nothing, 64 us.
 template <int DT, int EPI, int WM, int WN, int TM, int TN, int S>
 __global__ __launch_bounds__(WM * WN * 64, 1) void mx_gemm_kernel(const MxGemm g, const MxTiles tiles) {
     using P = MxPlan<WM, WN, TM, TN, S>;
@@ -369,13 +369,16 @@ static int run_mx_gemm(const MxGemm& g, long band, long most, hipStream_t st) {
 }
 
 // Which tile.  A workgroup of 128 x 128 takes 0.48 us for a step of 128 k when it has a compute unit to itself (instructions and latency, not the MFMAs), two
-// of them 0.62 us a step between them; one of 256 x 256 takes 1.0 us where the small tiles need 1.24 for as much.  Measured with fp16, M x K x N in us a call:
-//   256 x 256 from two tiles per compute unit on: 8192 x 8192 x 8192 255 (128 x 128: 321), 7168 x 4096 x 6144 114 (131), 16384 x 640 x 5120 60 (67 to
-//   77), 17071 x 6144 x 2048 133 (141), with a residual 8192 x 4096 x 4096 98 (105), 16384 x 1280 x 5120 130 (131); 4096 x 1280 x 10240 49 (48), with a
-//   residual 76 (68); with fewer tiles it loses: 16896 x 1536 x 1024 33 (25), 2964 x 1280 x 3840 18.2 (17.1).
-//   128 x 160 where that makes one round of what would be one and a part: 4096 x 1280 x 1280 + residual 12.1 (128 x 128: 13.8), 4096 x 5120 x 1280 24.0
-//   (26.4), 2461 x 320 x 1920 7.6 (8.0); in other places 10 to 30 % behind, since its four waves share no weights.
-// Several tiles to a workgroup: 16384 x 640 x 5120 76 where one each takes 82, 4096 x 1280 x 10240 48 (57).
+// of them 0.62 us a step between them; one of 256 x 256 takes 1.0 us where the small tiles need 1.24 for as much.  Measured with fp16, M x K x N in us a call
+// on activations in MXFP4:
+//   256 x 256 from two tiles per compute unit on: 8192 x 8192 x 8192 250 (128 x 128: 309), 7168 x 4096 x 6144 99 (109), 16384 x 1280 x 5120 75 (83),
+//   32768 x 320 x 2560 48 (57), with a residual 8192 x 4096 x 4096 91 (101), 16384 x 1280 x 5120 123 (139), 4096 x 1280 x 10240 69 (71).  Without a residual
+//   some are no faster, 4096 x 1280 x 10240 44 (44), 17071 x 6144 x 2048 127 (126), 16384 x 640 x 5120 56 (55), and few tiles of five steps slower: 4096 x
+//   640 x 10240 32 (29).  With fewer tiles it loses: 16896 x 1536 x 1024 31 (23), 2964 x 1280 x 3840 17.1 (14.2).
+//   128 x 160 where that makes one round of what would be one and a part: 4096 x 1280 x 1280 + residual 10.7 (128 x 128: 11.9), 4096 x 5120 x 1280 20.9
+//   (23.4), 2461 x 320 x 1920 6.3 (6.8); in other places behind, since its four waves share no weights: 2048 x 2048 x 2048 10.8 (9.3), 2964 x 1280 x 3840 20.2
+//   (14.2).
+// Several tiles to a workgroup: 16384 x 640 x 5120 54 where one each takes 62, 4096 x 1280 x 10240 43 (48).
 template <int DT>
 static int choose_mx_gemm(const MxGemm& g, hipStream_t st) {
     auto tiles = [&](long a, long w) { return ((g.a.groups + a - 1) / a) * ((g.w.groups + w - 1) / w); };

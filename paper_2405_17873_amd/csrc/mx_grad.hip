@@ -108,7 +108,7 @@ struct GradPlan {
 // A wave has its own part of the reduction (units wv, wv + NW, ...) and its own LDS, and waits for nobody until the sums of the waves are joined: no
 // weight is widened twice in a tile, and no operand is read from LDS by two waves.  128 x 128 results of a wave are what its registers hold; LDS holds
 // three units then.
-// Measured (bfloat16): 8192 x 8192 x 8192 1060 us, 1.04 PFLOP/s (a library product of 16-bit matrices reaches 1.37), on zeros 870: a fifth is power.  With
+// Measured (bfloat16): 8192 x 8192 x 8192 1030 to 1045 us, 1.06 PFLOP/s (a library product of 16-bit matrices reaches 1.37), on zeros 870: a fifth is power.  With
 // no loads from memory 790 us.  A unit (32 MFMAs, 1024 cycles) keeps LDS busy for about as long: loads write 41 KB, widened weights 32, reads fetch 73.
 template <int DT, int TM, int NW, int S>
 __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, const GradWork work) {
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(256) void mx_grad_align_kernel(const uint16_t* dy, 
 
 // The form for a problem: 32, 64 or 128 rows of a tile, and how the last round of tiles is cut, by what it is estimated to take: a launch, and for every
 // round of 256 workgroups a fixed part (filling the pipeline, joining the waves) and one per unit of a wave.  us, estimate (measured) for 32 / 64 / 128
-// rows: 308 x 2048 x 640 8.1 (7.5) / 9.9 (9.0) / 11.9 (11.7), 1000 x 992 x 1000 9.6 (9.1) / 11.9 (10.9) / 15 (14), 4096 x 1280 x 1280 43 (43) / 35 (35) /
+// rows: 308 x 2048 x 640 8.6 (7.5) / 9.9 (9.0) / 11.9 (11.7), 1000 x 992 x 1000 9.6 (9.1) / 11.9 (10.9) / 15 (14), 4096 x 1280 x 1280 43 (43) / 35 (35) /
 // 32 (32), 8 x 5120 x 20480 in six parts 22 (22) / 27 (26) / 37 (35).
 struct GradForm {
     int tm;

@@ -2,8 +2,8 @@
 //
 // A row is held in registers by 8, 16, 32 or 64 lanes, so that each has three to five vectors of eight consecutive values (320, 640 and 1280 columns fill
 // them without a rest), or by a workgroup (up to 16384 columns), and is read once: mean, then the sum of squared deviations from it, then the output.
-// All sums are taken in fp32.  Bound by memory.  us: forward 16384 x 640 8.0 (5.2 TB/s), 2964 x 1280 4.8, 32768 x 2048 39 (6.8 TB/s), into MXFP4 9.5, 5.6
-// and 39; backward 19.5 (4.3 TB/s with a residual), 10.9 and 79.  (One row per wave of 64 lanes whatever its length, before stores went through: forward 13.8,
+// All sums are taken in fp32.  Bound by memory.  us a call among others: forward 16384 x 640 9.0 (4.7 TB/s; 8.0 traced), 2964 x 1280 4.7, 32768 x 2048 43 (6.2
+// TB/s), into MXFP4 10.6, 5.4 and 47; backward 18.6 (4.5 TB/s with a residual), 11.8 and 80.  (One row per wave of 64 lanes whatever its length, before stores went through: forward 13.8,
 // 6.9, 50, when these took 10.4, 5.5, 41.)
 #include <type_traits>
 
