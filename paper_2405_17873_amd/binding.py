@@ -936,7 +936,7 @@ def mx_linear_grad_workspace_bytes(M: int, N: int, K: int) -> int:
 
 def mx_linear_grad(dy: torch.Tensor, w: MxTensor, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dX = dY . W, the gradient of mx_linear with respect to its input (the quantisation of X passed straight through).  ws: optional uint8
-    workspace of mx_linear_grad_workspace_bytes(M, N, K)."""
+    workspace of mx_linear_grad_workspace_bytes(M, N, K).  out shares nothing with dy."""
     if w.top is None:
         raise ValueError("weights without `top`: make them with mx_quantize_weights or mx_pack")
     if out is None and ws is None:
