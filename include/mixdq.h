@@ -464,6 +464,35 @@ int mq_layer_norm_grad(const void* dy, long lddy, const void* x, long ldx, int M
                        size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * Around the microscaled linears of a transformer block.  The conventions of the section above hold.
+ * ---------------------------------------------------------------------------------------------- */
+
+/* Host code: the rotation's table from the frequency of every pair (radians for one position) and the axis of positions that it goes by (0 .. 3).
+ * table_host [pairs][4]: a 64-bit fraction of a turn (low word, high word), the axis, 0; the caller copies it to the device, 16-byte aligned.  Angles are
+ * position times fraction modulo one turn, in integers: as exact for far positions as for near ones. */
+int mq_rotary_table(const double* freq_host, const int* axis_host, int pairs, uint32_t* table_host);
+
+/* Norm of every query and key head, and its rotation by position.  x [M, (q_heads + k_heads) head_dim] of dtype: a row's query heads, then its key heads (the
+ * first columns of a stacked q, k, v with its row stride; the values are left alone).
+ *   norm != 0: u = x w / sqrt(mean of x^2 over the head + eps), w [head_dim] q_weight or k_weight of param_dtype (MQ_F16, MQ_BF16, MQ_F32), nullable: 1.
+ *   norm == 0: u = x, no weights.
+ *   y: pair p < pairs of u, values (p, p + pairs) of the head or (2 p, 2 p + 1) if interleaved, turned by positions[m, axis p] times its frequency; the rest of u.
+ * positions [M, axes] of signed integers of position_bytes (4 or 8), rows ldpos apart, axes 1 .. 4; pairs == 0: no rotation, table and positions unused.
+ * y may be x.  fp32, rounded once.  head_dim a multiple of 8 up to 512, pairs a multiple of 4, q_heads and k_heads up to 4096 (one of them may be 0),
+ * M (q_heads + k_heads) below 2^31, otherwise MQ_ERR_BAD_SHAPE. */
+int mq_qk_norm_rope(const void* x, int M, int q_heads, int k_heads, int head_dim, long ldx, const void* q_weight, const void* k_weight, int param_dtype, float eps,
+                    int norm, const void* table, int pairs, int interleaved, const void* positions, int position_bytes, int axes, long ldpos, void* y, long ldy,
+                    int dtype, void* stream);
+
+/* Its gradient: dx, and the sums for the weights over rows and heads (fp32 [head_dim], each nullable; in a fixed order; zero without rows).  x: the input of the
+ * forward call (unused, may be null, if norm == 0: then there are no weights either).  dx may be dy or x.  The workspace is for the sums of the weights only. */
+size_t mq_qk_norm_rope_grad_workspace_bytes(int M, int q_heads, int k_heads, int head_dim);
+int mq_qk_norm_rope_grad(const void* dy, long lddy, const void* x, int M, int q_heads, int k_heads, int head_dim, long ldx, const void* q_weight,
+                         const void* k_weight, int param_dtype, float eps, int norm, const void* table, int pairs, int interleaved, const void* positions,
+                         int position_bytes, int axes, long ldpos, void* dx, long lddx, int dtype, float* dq_weight, float* dk_weight, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/* ------------------------------------------------------------------------------------------------
  * Bit-width allocation (host only: every pointer in this section is a HOST pointer, no GPU is touched, nothing is
  * enqueued).  It produces the per-layer `bits` that the entry points above take.
  * ---------------------------------------------------------------------------------------------- */

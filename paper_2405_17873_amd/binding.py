@@ -62,7 +62,7 @@ def load():
             raise RuntimeError(f"{_LIB_PATH} is missing: run `python -c 'import __graft_entry__ as g; g.build()'`")
         lib = C.CDLL(_LIB_PATH)
         for name in ("mq_a8_row_bytes", "mq_split_workspace_bytes", "mq_builtin_workspace_bytes", "mq_conv3x3_a8_workspace_bytes", "mq_packed_bytes", "mq_qlinear_a8_workspace_bytes", "mq_qlinear_a8_geglu_dynamic_workspace_bytes", "mq_bos_aware_kv_proj_workspace_bytes",
-                     "mq_mx_bytes", "mq_mx_linear_workspace_bytes", "mq_mx_linear_grad_workspace_bytes", "mq_layer_norm_grad_workspace_bytes"):
+                     "mq_mx_bytes", "mq_mx_linear_workspace_bytes", "mq_mx_linear_grad_workspace_bytes", "mq_layer_norm_grad_workspace_bytes", "mq_qk_norm_rope_grad_workspace_bytes"):
             getattr(lib, name).restype = C.c_size_t
         lib.mq_prof_bracket_overhead_us.restype = C.c_double
         _lib = lib
@@ -1030,3 +1030,118 @@ def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Te
                                      _ptr(dx), _ld(dx), _dtype_code(x), _ptr(sums[0]), _ptr(sums[1]), _ptr(ws), _bytes_of(ws), _stream()),
            "mq_layer_norm_grad")
     return dx, sums[0], sums[1]
+
+
+# ------------------------------------------------------------- around the microscaled linears of a transformer block
+
+
+def _on_current(device) -> None:
+    """Kernels are launched on the current device's stream."""
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"operands are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+@dataclass
+class Rotary:
+    """Rotation of the first 2 `pairs` values of a head: of pair p by positions[:, axis p] times its frequency.  Made by rotary()."""
+    table: torch.Tensor   # int32 [pairs, 4] on the GPU: a 64-bit fraction of a turn, the axis, 0
+    pairs: int
+    axes: int
+    interleaved: bool     # pairs (2 p, 2 p + 1); otherwise (p, p + pairs)
+
+
+def rotary(sections, theta: float = 10000.0, interleaved: bool = False, device=None, freqs=None, restart: bool = True) -> Rotary:
+    """sections: pairs of each of one to four axes of positions (the pairs of the first axis come first; a multiple of four in all).  Frequencies are
+    theta^(-i / n) over the n pairs of an axis, restart=False: over all pairs; freqs: given ones (radians for one position), as many as pairs."""
+    import numpy as np
+
+    sections = [int(n) for n in sections]
+    pairs = sum(sections)
+    if not 1 <= len(sections) <= 4 or min(sections) < 0 or pairs == 0 or pairs % 4:
+        raise ValueError(f"a rotation has one to four axes, and a multiple of four pairs in all, got {sections}")
+    if freqs is None:
+        freqs = [theta ** (-i / n) for n in sections for i in range(n)] if restart else [theta ** (-i / pairs) for i in range(pairs)]
+    freq = np.ascontiguousarray([float(f) for f in freqs], np.float64)
+    if freq.shape != (pairs,):
+        raise ValueError(f"{pairs} pairs, {freq.shape[0]} frequencies")
+    axis = np.repeat(np.arange(len(sections), dtype=np.int32), sections)
+    table = np.zeros((pairs, 4), np.int32)
+    _check(load().mq_rotary_table(_np_ptr(freq), _np_ptr(axis), pairs, _np_ptr(table)), "mq_rotary_table")
+    device = torch.device("cuda" if device is None else device)
+    return Rotary(torch.from_numpy(table).to(device), pairs, len(sections), bool(interleaved))
+
+
+def _head_args(x: torch.Tensor, q_heads: int, k_heads: int, q_weight, k_weight, rot: Optional[Rotary], positions, eps, norm: bool):
+    """Arguments from the sizes to the positions, checked; what they point to has to live until the call."""
+    M, cols = x.shape
+    heads = int(q_heads) + int(k_heads)
+    if q_heads < 0 or k_heads < 0 or heads == 0 or cols % heads:
+        raise ValueError(f"{cols} columns are no {q_heads} query and {k_heads} key heads")
+    D = cols // heads
+    if not norm and (q_weight is not None or k_weight is not None):
+        raise ValueError("weights without the norm")
+    p = q_weight if q_weight is not None else k_weight
+    for t in (q_weight, k_weight):
+        _vector(t, D, None if p is None else p.dtype, x.device)
+    pt = F32 if p is None or p.dtype == torch.float32 else _dtype_code(p)
+    if (rot is None) != (positions is None):
+        raise ValueError("a rotation goes with positions")
+    if rot is None:
+        turn = (None, 0, 0, None, 4, 0, C.c_long(0))
+    else:
+        pos = positions if positions.dim() == 2 else positions.unsqueeze(-1)
+        if pos.dim() != 2 or tuple(pos.shape) != (M, rot.axes) or pos.device != x.device:
+            raise ValueError(f"expected positions [{M}, {rot.axes}] on {x.device}, got {tuple(positions.shape)} on {positions.device}")
+        if pos.dtype not in (torch.int32, torch.int64):
+            raise TypeError(f"positions are int32 or int64, got {pos.dtype}")
+        if (rot.axes > 1 and pos.stride(1) != 1) or (M > 1 and pos.stride(0) < rot.axes):
+            pos = pos.contiguous()
+        if rot.table.device != x.device or rot.table.dtype != torch.int32 or tuple(rot.table.shape) != (rot.pairs, 4) or not rot.table.is_contiguous():
+            raise ValueError(f"expected a rotation's table on {x.device}, got {tuple(rot.table.shape)} of {rot.table.dtype} on {rot.table.device}")
+        turn = (_ptr(rot.table), rot.pairs, int(rot.interleaved), _ptr(pos), pos.element_size(), rot.axes, C.c_long(pos.stride(0) if M > 1 else rot.axes))
+        positions = pos
+    return (M, int(q_heads), int(k_heads), D, _ld(x), _ptr(q_weight), _ptr(k_weight), pt, C.c_float(eps), int(norm), *turn), positions
+
+
+def qk_norm_rope(x: torch.Tensor, q_heads: int, k_heads: int, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                 rotary: Optional[Rotary] = None, positions: Optional[torch.Tensor] = None, eps: float = 1e-6, norm: bool = True,
+                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Norm of every query and key head, x w / sqrt(mean x^2 + eps), and its rotation by position.  x [M, (q_heads + k_heads) D] fp16/bf16: a row's
+    query heads, then its key heads (of a stacked q, k, v the columns in front of the values: qkv[:, :n], with out the same to work in place).  q_weight, k_weight [D]
+    in 16 bits or float32.  rotary: from rotary(); positions: int32 or int64 [M, axes], [M] for one axis.  norm=False: the rotation alone.  out may be x."""
+    _no_graph("qk_norm_rope", x, q_weight, k_weight)
+    _matrix(x)
+    _on_current(x.device)
+    dt = _dtype_code(x)
+    args, positions = _head_args(x, q_heads, k_heads, q_weight, k_weight, rotary, positions, eps, norm)
+    y = _out(out, *x.shape, x.dtype, x.device)
+    _check(load().mq_qk_norm_rope(_ptr(x), *args, _ptr(y), _ld(y), dt, _stream()), "mq_qk_norm_rope")
+    return y
+
+
+def qk_norm_rope_grad_workspace_bytes(M: int, q_heads: int, k_heads: int, D: int) -> int:
+    return int(load().mq_qk_norm_rope_grad_workspace_bytes(M, q_heads, k_heads, D))
+
+
+def qk_norm_rope_grad(dy: torch.Tensor, x: Optional[torch.Tensor], q_heads: int, k_heads: int, q_weight: Optional[torch.Tensor] = None,
+                      k_weight: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None, positions: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                      norm: bool = True, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """(dx, dq_weight, dk_weight) of qk_norm_rope, x its input; the latter two float32 [D], sums over rows and heads, None without a norm (which needs no x
+    either).  out may be dy or x."""
+    _no_graph("qk_norm_rope_grad", dy)
+    _matrix(dy)
+    _on_current(dy.device)
+    dt = _dtype_code(dy)
+    if norm:
+        _matrix(x, *dy.shape, dy.dtype, dy.device)
+    else:
+        x = None
+    args, positions = _head_args(dy if x is None else x, q_heads, k_heads, q_weight, k_weight, rotary, positions, eps, norm)
+    M, D = args[0], args[3]
+    dx = _out(out, *dy.shape, dy.dtype, dy.device)
+    sums = torch.empty((2, D), dtype=torch.float32, device=dy.device) if norm else None
+    ws = _mx_workspace(qk_norm_rope_grad_workspace_bytes(M, q_heads, k_heads, D), dy.device, ws) if norm else None
+    dq, dk = (None, None) if sums is None else (sums[0], sums[1])
+    _check(load().mq_qk_norm_rope_grad(_ptr(dy), _ld(dy), _ptr(x), *args, _ptr(dx), _ld(dx), dt, _ptr(dq), _ptr(dk), *_ws_args(ws), _stream()),
+           "mq_qk_norm_rope_grad")
+    return dx, dq, dk

@@ -2,6 +2,7 @@
 files are cached per source; pass force=True to rebuild everything."""
 from __future__ import annotations
 
+import glob
 import os
 import subprocess
 import sys
@@ -29,16 +30,16 @@ PER_FILE = {
     "gemm_solo.hip": ["-fno-slp-vectorize"],
     "gemm_panel.hip": ["-fno-slp-vectorize", "-ffp-contract=off"],
     "norm.hip": ["-fno-slp-vectorize"],
+    "heads.hip": ["-fno-slp-vectorize"],
 }
 SOURCES = ["api.hip", "quant_pack.hip", "act_quant.hip", "gemm.hip", "gemm_solo.hip", "gemm_panel.hip", "bos.hip", "prof.hip", "peaks.hip", "alloc.cpp",
-           "mx_quant.hip", "mx_gemm.hip", "mx_rows.hip", "mx_grad.hip", "norm.hip", "api_mx.hip"]
+           "mx_quant.hip", "mx_gemm.hip", "mx_rows.hip", "mx_grad.hip", "norm.hip", "heads.hip", "api_mx.hip", "api_block.hip"]
 
 
 def _compile(src: str, force: bool) -> str:
     path = os.path.join(CSRC, src)
     obj = os.path.join(OBJ, src + ".o")
-    deps = [path, os.path.join(CSRC, "mq_common.h"), os.path.join(CSRC, "bos_rows.h"), os.path.join(CSRC, "gemm_core.h"), os.path.join(CSRC, "act_range.h"), os.path.join(CSRC, "mx_common.h"), os.path.join(CSRC, "per_device.h"),
-            os.path.join(HERE, "..", "include", "mixdq.h"), __file__]
+    deps = [path, *glob.glob(os.path.join(CSRC, "*.h")), os.path.join(HERE, "..", "include", "mixdq.h"), __file__]
     if not force and os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
         return obj
     cmd = [HIPCC, *COMMON, *EXTRA, *PER_FILE.get(src, []), "-c", path, "-o", obj]

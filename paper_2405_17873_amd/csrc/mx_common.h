@@ -203,6 +203,40 @@ struct NormArgs {
     float* dbias;    // nullable
     float* partial;  // workspace
 };
+// Query and key heads: x [M, (q + k) D], rows of heads.
+struct HeadArgs {
+    const uint16_t* x;
+    long ldx;
+    int M, q, k, D;
+    const void *qw, *kw;  // nullable: 1
+    int param_dtype;
+    float eps;
+    bool norm;
+    const uint4v* table;  // of every pair: fraction of a turn for one position (low word, high word), axis
+    int pairs;            // 0: no rotation
+    bool interleaved;
+    const void* pos;  // [M, axes], 4 or 8 bytes each
+    int pos_bytes, axes;
+    long ldpos;
+    int dtype;
+    // forward
+    uint16_t* y;
+    long ldy;
+    // backward
+    const uint16_t* dy;
+    long lddy;
+    uint16_t* dx;
+    long lddx;
+    float *dq_weight, *dk_weight;  // nullable
+    float* partial;                // workspace
+    // set by the launcher: chunks of a row's heads, heads in each, waves' tasks in all
+    FastDiv chunks;
+    int per_chunk;
+    uint32_t tasks;
+};
+int launch_heads(HeadArgs& a, bool grad, hipStream_t st);
+size_t heads_grad_workspace_bytes(long M, int H, int D);
+
 int launch_layer_norm(const NormArgs& a, hipStream_t st);
 int launch_layer_norm_mx(const NormArgs& a, hipStream_t st);
 size_t layer_norm_grad_workspace_bytes(long M, long C);
