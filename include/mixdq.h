@@ -49,6 +49,11 @@ extern "C" {
 #define MQ_F16 0
 #define MQ_BF16 1
 #define MQ_F32 2 /* parameters of the layer norm only */
+/* Activations (act): none, a Phi(a), its tanh approximation, a / (1 + exp(-a)). */
+#define MQ_ACT_NONE 0
+#define MQ_ACT_GELU 1
+#define MQ_ACT_GELU_TANH 2
+#define MQ_ACT_SILU 3
 
 /* Library version and the last HIP error code seen by a failing call (0 if none). */
 int mq_version(void);
@@ -491,6 +496,37 @@ int mq_qk_norm_rope_grad(const void* dy, long lddy, const void* x, int M, int q_
                          const void* k_weight, int param_dtype, float eps, int norm, const void* table, int pairs, int interleaved, const void* positions,
                          int position_bytes, int axes, long ldpos, void* dx, long lddx, int dtype, float* dq_weight, float* dk_weight, void* ws, size_t ws_bytes,
                          void* stream);
+
+/* mq_mx_linear with an activation behind it: a = mx(X) W^T + bias, Y = act(a) (+ residual), act one of MQ_ACT_*.  gated: Y [M, N / 2] = v act(g), v and g the
+ * first and the second half of a's columns (N % 64 == 0, N K <= 2^32, no residual, act not MQ_ACT_NONE).  pre [M,N] of dtype, nullable: a, rounded, for mq_act_grad;
+ * apart from Y and residual.  a's float32 values go into the activation.  Y and pre may overlap X.  The workspace is mq_mx_linear's (if X overlaps Y or pre:
+ * mq_mx_bytes(M, K)). */
+int mq_mx_linear_act(const void* x, int M, int K, long ldx, const void* w, int N, const void* bias, int act, int gated, void* y, long ldy, int dtype,
+                     const void* residual, long ldr, void* pre, long ldpre, void* ws, size_t ws_bytes, void* stream);
+int mq_mx_linear_act_codes(const void* a, int M, int K, const void* w, int N, const void* bias, int act, int gated, void* y, long ldy, int dtype,
+                           const void* residual, long ldr, void* pre, long ldpre, void* stream);
+
+/* Gradient behind the activation: pre [M,N] of dtype (a of the forward call), dY [M,N] (gated [M, N / 2], N even) -> da [M,N]: dY act'(a), gated dY act(g) and
+ * dY v act'(g); and dbias [N] (fp32, nullable; zero without rows), the sums over the rows of da's float32 values in a fixed order.  da is what mq_mx_linear_grad
+ * takes.  da may be pre, and dY if not gated.  The workspace is for dbias only. */
+size_t mq_act_grad_workspace_bytes(int M, int N, int gated);
+int mq_act_grad(const void* dy, int M, int N, long lddy, const void* pre, long ldpre, int act, int gated, void* da, long ldda, int dtype, float* dbias, void* ws,
+                size_t ws_bytes, void* stream);
+
+/* Products by expert.  w: the microscaled matrices of `experts` experts, N rows each (N % 32 == 0), as one matrix of experts * N rows.  Rows offsets[e] ..
+ * offsets[e + 1] - 1 of X are expert e's: offsets [experts + 1] (on the GPU) rise from 0 .. to .. M, and an expert may have none; what they hold otherwise is held
+ * at what came before, and the results of rows that belong to two experts are undefined.  Rows before offsets[0] and from offsets[experts] on are left as they were.
+ * bias [experts, N] of dtype, nullable; act, gated and pre as above; Y, pre and X share nothing.  Each result is that of mq_mx_linear_act with its expert's weights.
+ * Up to 4096 experts, 2^28 rows of X and of w. */
+size_t mq_mx_linear_grouped_workspace_bytes(int M, int N, int K, int experts); /* 0: none is needed, ws may be null */
+int mq_mx_linear_grouped(const void* x, int M, int K, long ldx, const void* w, int N, int experts, const int* offsets, const void* bias, int act, int gated,
+                         void* y, long ldy, int dtype, void* pre, long ldpre, void* ws, size_t ws_bytes, void* stream);
+
+/* dX = dY W_e for the rows of each expert, as mq_mx_linear_grad; top [experts, K / 32] from mq_mx_experts_column_top. */
+int mq_mx_experts_column_top(const void* mx, int experts, int N, int K, uint8_t* top, void* stream);
+size_t mq_mx_linear_grouped_grad_workspace_bytes(int M, int experts);
+int mq_mx_linear_grouped_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, int experts, const int* offsets, void* dx,
+                              long lddx, int dtype, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Bit-width allocation (host only: every pointer in this section is a HOST pointer, no GPU is touched, nothing is

@@ -62,7 +62,8 @@ def load():
             raise RuntimeError(f"{_LIB_PATH} is missing: run `python -c 'import __graft_entry__ as g; g.build()'`")
         lib = C.CDLL(_LIB_PATH)
         for name in ("mq_a8_row_bytes", "mq_split_workspace_bytes", "mq_builtin_workspace_bytes", "mq_conv3x3_a8_workspace_bytes", "mq_packed_bytes", "mq_qlinear_a8_workspace_bytes", "mq_qlinear_a8_geglu_dynamic_workspace_bytes", "mq_bos_aware_kv_proj_workspace_bytes",
-                     "mq_mx_bytes", "mq_mx_linear_workspace_bytes", "mq_mx_linear_grad_workspace_bytes", "mq_layer_norm_grad_workspace_bytes", "mq_qk_norm_rope_grad_workspace_bytes"):
+                     "mq_mx_bytes", "mq_mx_linear_workspace_bytes", "mq_mx_linear_grad_workspace_bytes", "mq_layer_norm_grad_workspace_bytes", "mq_qk_norm_rope_grad_workspace_bytes", "mq_act_grad_workspace_bytes",
+                     "mq_mx_linear_grouped_workspace_bytes", "mq_mx_linear_grouped_grad_workspace_bytes"):
             getattr(lib, name).restype = C.c_size_t
         lib.mq_prof_bracket_overhead_us.restype = C.c_double
         _lib = lib
@@ -746,11 +747,13 @@ _HALF = (None, torch.float16)  # mx_linear's default
 
 @dataclass
 class MxTensor:
-    """A [rows, K] matrix in microscaled 4-bit floats, in the product's form.  top: for weights whose layer is differentiated."""
+    """A [rows, K] matrix in microscaled 4-bit floats, in the product's form.  top: for weights whose layer is differentiated.  experts: of as many
+    experts' weights, one's rows behind another's."""
     data: torch.Tensor                  # uint8, mx_bytes(rows, K)
     rows: int
     K: int
-    top: Optional[torch.Tensor] = None  # uint8 [K / 32], the largest scale of every column of blocks
+    top: Optional[torch.Tensor] = None  # uint8 [K / 32], the largest scale of every column of blocks (of each expert)
+    experts: int = 1
 
     @property
     def shape(self):
@@ -889,9 +892,14 @@ def mx_linear_workspace_bytes(M: int, N: int, K: int) -> int:
 
 
 def mx_linear(x: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-              residual: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, dtype=None) -> torch.Tensor:
+              residual: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, dtype=None, act: Optional[str] = None, gated: bool = False,
+              want_pre: bool = False):
     """Y = mx(X) . W^T + bias (+ residual).  X: [M, K] fp16/bf16, quantised in the call, or an MxTensor; then dtype (fp16 unless out or
-    dtype says otherwise) is the output's.  residual may be out itself.  ws: optional uint8 workspace of mx_linear_workspace_bytes(M, N, K)."""
+    dtype says otherwise) is the output's.  residual may be out itself.  ws: optional uint8 workspace of mx_linear_workspace_bytes(M, N, K).
+    act: "gelu", "gelu_tanh" or "silu", Y = act(mx(X) . W^T + bias) (+ residual).  gated: Y [M, N / 2] = v act(g), v and g the first and the second half of the
+    columns, N % 64 == 0, no residual.  want_pre: (Y, mx(X) . W^T + bias [M, N]), the latter for act_grad."""
+    if act is not None or gated or want_pre:
+        return _mx_linear_act(x, w, bias, out, residual, ws, dtype, act, gated, want_pre)
     packed = isinstance(x, MxTensor)
     if out is None and ws is None:
         native = _native or _load_native()
@@ -1145,3 +1153,154 @@ def qk_norm_rope_grad(dy: torch.Tensor, x: Optional[torch.Tensor], q_heads: int,
     _check(load().mq_qk_norm_rope_grad(_ptr(dy), _ld(dy), _ptr(x), *args, _ptr(dx), _ld(dx), dt, _ptr(dq), _ptr(dk), *_ws_args(ws), _stream()),
            "mq_qk_norm_rope_grad")
     return dx, dq, dk
+
+
+_ACTS = {None: 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
+
+
+def _act_code(act: Optional[str], gated: bool) -> int:
+    if act not in _ACTS:
+        raise ValueError(f"activations are gelu, gelu_tanh and silu, got {act!r}")
+    if gated and act is None:
+        raise ValueError("a gate has an activation")
+    return _ACTS[act]
+
+
+def _pre_out(want: bool, rows: int, cols: int, dtype, device):
+    return torch.empty((rows, cols), dtype=dtype, device=device) if want else None
+
+
+def _mx_linear_act(x, w: MxTensor, bias, out, residual, ws, dtype, act, gated: bool, want_pre: bool):
+    packed = isinstance(x, MxTensor)
+    if act is None:
+        raise ValueError("gated and want_pre go with an activation")
+    code = _act_code(act, gated)
+    _no_graph("mx_linear", None if packed else x, bias, residual)
+    if packed:
+        M, K, device = x.rows, x.K, x.data.device
+        dtype = dtype or (out.dtype if out is not None else torch.float16)
+    else:
+        (M, K), device = _matrix(x).shape, x.device
+        if dtype is not None and dtype != x.dtype:
+            raise TypeError(f"the output has the type of the activations, {x.dtype}")
+        dtype = x.dtype
+    _on_current(device)
+    if K != w.K:
+        raise ValueError(f"activations have {K} columns, weights {w.K}")
+    if gated and (w.rows % 64 or residual is not None):
+        raise ValueError(f"a gate takes a multiple of 64 rows of weights and no residual, got {w.rows}")
+    N = w.rows
+    outs = N // 2 if gated else N
+    y = _out(out, M, outs, dtype, device)
+    dt = _dtype_code(y)
+    pre = _pre_out(want_pre, M, N, dtype, device)
+    if residual is not None:
+        _matrix(residual, M, outs, dtype, device)
+    args = (_mx_data(w, device), N, _ptr(_vector(bias, N, dtype, device)), code, int(gated), _ptr(y), _ld(y), dt, _ptr(residual), _ld(residual), _ptr(pre), _ld(pre))
+    if packed:
+        _check(load().mq_mx_linear_act_codes(_mx_data(x, device), M, K, *args, _stream()), "mq_mx_linear_act_codes")
+    else:
+        ws = _mx_workspace(mx_linear_workspace_bytes(M, N, K) or (0 if out is None else mx_bytes(M, K)), device, ws)
+        _check(load().mq_mx_linear_act(_ptr(x), M, K, _ld(x), *args, _ptr(ws), _bytes_of(ws), _stream()), "mq_mx_linear_act")
+    return (y, pre) if want_pre else y
+
+
+def act_grad_workspace_bytes(M: int, N: int, gated: bool = False) -> int:
+    return int(load().mq_act_grad_workspace_bytes(M, N, int(gated)))
+
+
+def act_grad(dy: torch.Tensor, pre: torch.Tensor, act: str, gated: bool = False, want_dbias: bool = True, out: Optional[torch.Tensor] = None,
+             ws: Optional[torch.Tensor] = None):
+    """(da, dbias): the gradient of mx_linear's sums behind its activation, which mx_linear_grad takes, and the bias' (float32 [N], None without want_dbias).
+    pre [M, N]: from want_pre.  dy [M, N], gated [M, N / 2].  out may be pre, and dy if not gated."""
+    code = _act_code(act, gated)
+    if not code:
+        raise ValueError("act_grad is behind an activation")
+    _no_graph("act_grad", dy, pre)
+    M, N = _matrix(pre).shape
+    _on_current(pre.device)
+    if gated and N % 2:
+        raise ValueError(f"a gate has two halves, got {N} columns")
+    _matrix(dy, M, N // 2 if gated else N, pre.dtype, pre.device)
+    da = _out(out, M, N, pre.dtype, pre.device)
+    dbias = torch.empty(N, dtype=torch.float32, device=pre.device) if want_dbias else None
+    ws = _mx_workspace(act_grad_workspace_bytes(M, N, gated), pre.device, ws) if want_dbias else None
+    _check(load().mq_act_grad(_ptr(dy), M, N, _ld(dy), _ptr(pre), _ld(pre), code, int(gated), _ptr(da), _ld(da), _dtype_code(pre), _ptr(dbias), *_ws_args(ws),
+                              _stream()), "mq_act_grad")
+    return da, dbias
+
+
+def mx_experts(t: MxTensor, experts: int) -> MxTensor:
+    """A microscaled matrix as the weights of `experts` experts, one's rows behind another's, a multiple of 32 rows each; with what the gradient needs."""
+    if experts <= 0 or t.rows % (32 * experts):
+        raise ValueError(f"{t.rows} rows are no {experts} experts of a multiple of 32 rows")
+    data = _mx_data(t)
+    top = torch.empty((experts, t.K // 32), dtype=torch.uint8, device=t.data.device)
+    _check(load().mq_mx_experts_column_top(data, experts, t.rows // experts, t.K, _ptr(top), _stream()), "mq_mx_experts_column_top")
+    return MxTensor(t.data, t.rows, t.K, top, experts)
+
+
+def mx_quantize_experts(w: torch.Tensor) -> MxTensor:
+    """Weights [experts, N, K] fp16/bf16, N % 32 == 0, for mx_linear_grouped and its gradient."""
+    if w.dim() != 3:
+        raise ValueError(f"expected weights [experts, N, K], got {tuple(w.shape)}")
+    return mx_experts(mx_quantize(w.reshape(w.shape[0] * w.shape[1], w.shape[2])), w.shape[0])
+
+
+def _expert_args(M: int, w: MxTensor, offsets: torch.Tensor, device):
+    if w.experts <= 0 or w.rows % (32 * w.experts):
+        raise ValueError(f"{w.rows} rows are no {w.experts} experts of a multiple of 32 rows")
+    _vector(offsets, w.experts + 1, torch.int32, device)
+    return w.rows // w.experts
+
+
+def mx_linear_grouped_workspace_bytes(M: int, N: int, K: int, experts: int) -> int:
+    return int(load().mq_mx_linear_grouped_workspace_bytes(M, N, K, experts))
+
+
+def mx_linear_grouped(x: torch.Tensor, w: MxTensor, offsets: torch.Tensor, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None, act: Optional[str] = None, gated: bool = False, want_pre: bool = False):
+    """Rows sorted by expert, each expert's times its own weights: Y[r] = mx(X[r]) . W_e^T + bias[e] for offsets[e] <= r < offsets[e + 1]; act, gated and
+    want_pre as in mx_linear.  w: from mx_quantize_experts or mx_experts; offsets: int32 [experts + 1] on the GPU, never read on the host; bias [experts, N].  Rows that
+    no expert has are left as they are in out (and hold nothing in particular otherwise).  out shares nothing with x."""
+    code = _act_code(act, gated)
+    if want_pre and act is None:
+        raise ValueError("want_pre goes with an activation")
+    _no_graph("mx_linear_grouped", x, bias)
+    M, K = _matrix(x).shape
+    device = x.device
+    _on_current(device)
+    if K != w.K:
+        raise ValueError(f"activations have {K} columns, weights {w.K}")
+    N = _expert_args(M, w, offsets, device)
+    if gated and N % 64:
+        raise ValueError(f"a gate takes a multiple of 64 rows of weights, got {N}")
+    if bias is not None and (tuple(bias.shape) != (w.experts, N) or not bias.is_contiguous() or bias.dtype != x.dtype or bias.device != device):
+        raise ValueError(f"expected a contiguous bias [{w.experts}, {N}] of {x.dtype} on {device}, got {tuple(bias.shape)} of {bias.dtype} on {bias.device}")
+    y = _out(out, M, N // 2 if gated else N, x.dtype, device)
+    pre = _pre_out(want_pre, M, N, x.dtype, device)
+    ws = _mx_workspace(mx_linear_grouped_workspace_bytes(M, N, K, w.experts), device, ws)
+    _check(load().mq_mx_linear_grouped(_ptr(x), M, K, _ld(x), _mx_data(w, device), N, w.experts, _ptr(offsets), _ptr(bias), code, int(gated), _ptr(y), _ld(y),
+                                       _dtype_code(x), _ptr(pre), _ld(pre), *_ws_args(ws), _stream()), "mq_mx_linear_grouped")
+    return (y, pre) if want_pre else y
+
+
+def mx_linear_grouped_grad_workspace_bytes(M: int, experts: int) -> int:
+    return int(load().mq_mx_linear_grouped_grad_workspace_bytes(M, experts))
+
+
+def mx_linear_grouped_grad(dy: torch.Tensor, w: MxTensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
+                           ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dX[r] = dY[r] . W_e, the gradient of mx_linear_grouped with respect to its rows (the quantisation passed straight through).  out shares nothing with dy."""
+    _no_graph("mx_linear_grouped_grad", dy)
+    M, N = _matrix(dy).shape
+    _on_current(dy.device)
+    if _expert_args(M, w, offsets, dy.device) != N:
+        raise ValueError(f"gradients have {N} columns, an expert's weights {w.rows // w.experts} rows")
+    if w.top is None or w.top.numel() != w.experts * (w.K // 32) or w.top.dtype != torch.uint8 or not w.top.is_contiguous() or w.top.device != dy.device:
+        raise ValueError("weights without the experts' `top`: make them with mx_quantize_experts or mx_experts")
+    dx = _out(out, M, w.K, dy.dtype, dy.device)
+    ws = _mx_workspace(mx_linear_grouped_grad_workspace_bytes(M, w.experts), dy.device, ws)
+    _check(load().mq_mx_linear_grouped_grad(_ptr(dy), M, N, _ld(dy), _mx_data(w, dy.device), _ptr(w.top), w.K, w.experts, _ptr(offsets), _ptr(dx), _ld(dx),
+                                            _dtype_code(dy), *_ws_args(ws), _stream()), "mq_mx_linear_grouped_grad")
+    return dx

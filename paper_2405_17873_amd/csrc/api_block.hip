@@ -28,6 +28,47 @@ static HeadArgs head_args(const void* x, int M, int q, int k, int D, long ldx, c
     return a;
 }
 
+// What a product with an activation or a gate (N rows of weights for N / 2 columns of Y) has beside one without.
+static int check_act(int M, int N, int act, int gated, const void* y, long ldy, const void* residual, const void* pre, long ldpre) {
+    if (act < MQ_ACT_NONE || act > MQ_ACT_SILU || (gated && (act == MQ_ACT_NONE || residual))) return MQ_ERR_BAD_ARG;
+    if (gated && N % 64 != 0) return MQ_ERR_BAD_SHAPE;
+    if (pre)
+        if (const int rc = check_matrix(pre, M, ldpre, N)) return rc;
+    if (M > 0 && pre && !apart(pre, ldpre, N, y, ldy, gated ? N / 2 : N, M)) return MQ_ERR_BAD_ARG;
+    return MQ_OK;
+}
+// (offsets of a gate's weights behind its values' are 32-bit)
+static bool gate_fits(int N, int K) { return (long)N * K <= 1L << 32; }
+static int check_product_act(int M, int N, int K, const void* w, const void* bias, int act, int gated, const void* y, long ldy, int dtype, const void* residual,
+                             long ldr, const void* pre, long ldpre) {
+    int rc;
+    if (N <= 0 || N > (1 << 22) || (gated && N % 64 != 0)) return MQ_ERR_BAD_SHAPE;
+    const int outs = gated ? N / 2 : N;
+    if ((rc = check_product(M, outs, K, w, bias, y, ldy, dtype, residual, ldr)) || (rc = check_mx(w, N, K)) ||
+        (rc = check_act(M, N, act, gated, y, ldy, residual, pre, ldpre)))
+        return rc;
+    if (gated && !gate_fits(N, K)) return MQ_ERR_BAD_SHAPE;
+    if (M > 0 && !itself_or_apart(y, ldy, residual, ldr, outs, M)) return MQ_ERR_BAD_ARG;
+    if (M > 0 && pre && residual && !apart(pre, ldpre, N, residual, ldr, N, M)) return MQ_ERR_BAD_ARG;
+    return MQ_OK;
+}
+static MxGemm product_act(int M, int K, const void* w, int N, const void* bias, int act, void* y, long ldy, int dtype, const void* residual, long ldr, void* pre,
+                          long ldpre) {
+    MxGemm g = product(M, K, w, N, bias, y, ldy, dtype, residual, ldr);
+    g.act = act, g.pre = (uint16_t*)pre, g.ldpre = ldpre;
+    return g;
+}
+static int run_act(MxGemm& g, int gated, const void* a, hipStream_t st) {
+    g.a = mx_view(a, g.M, g.K);
+    return mx_rows_takes(g.M, g.N) ? launch_mx_rows_act(g, gated, nullptr, 0, st) : launch_mx_gemm_act(g, gated, st);
+}
+// Weights of `experts` experts, N rows of each, one behind the other in one matrix.
+static int check_experts(const void* w, int N, int K, int experts, const int* offsets, int M) {
+    if (experts <= 0 || experts > 4096 || N <= 0 || N > (1 << 22) || N % 32 != 0 || (long)N * experts > 1 << 28 || M > (1 << 28)) return MQ_ERR_BAD_SHAPE;
+    if (!offsets || !aligned(offsets, 4)) return MQ_ERR_BAD_ARG;
+    return check_mx(w, N * experts, K);
+}
+
 }  // namespace mq
 
 using namespace mq;
@@ -95,6 +136,102 @@ int mq_qk_norm_rope_grad(const void* dy, long lddy, const void* x, int M, int q_
                            axes, ldpos, dtype);
     a.dy = (const uint16_t*)dy, a.lddy = lddy, a.dx = (uint16_t*)dx, a.lddx = lddx, a.dq_weight = dq_weight, a.dk_weight = dk_weight, a.partial = (float*)ws;
     return launch_heads(a, true, (hipStream_t)stream);
+}
+
+int mq_mx_linear_act(const void* x, int M, int K, long ldx, const void* w, int N, const void* bias, int act, int gated, void* y, long ldy, int dtype,
+                     const void* residual, long ldr, void* pre, long ldpre, void* ws, size_t ws_bytes, void* stream) {
+    int rc;
+    if ((rc = check_product_act(M, N, K, w, bias, act, gated, y, ldy, dtype, residual, ldr, pre, ldpre)) || (rc = check_matrix(x, M, ldx, K))) return rc;
+    if (M == 0) return MQ_OK;
+    MxGemm g = product_act(M, K, w, N, bias, act, y, ldy, dtype, residual, ldr, pre, ldpre);
+    // (one launch reads activations while others of its workgroups store results)
+    if (mx_rows_quantizes(M, N, K) && apart(x, ldx, K, y, ldy, gated ? N / 2 : N, M) && (!pre || apart(x, ldx, K, pre, ldpre, N, M)))
+        return launch_mx_rows_act(g, gated, x, ldx, (hipStream_t)stream);
+    if (!ws || !aligned(ws, 256)) return MQ_ERR_BAD_ARG;
+    if (ws_bytes < up256(mx_bytes(M, K))) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    if ((rc = launch_mx_quantize(x, M, K, ldx, dtype, ws, (hipStream_t)stream))) return rc;
+    return run_act(g, gated, ws, (hipStream_t)stream);
+}
+
+int mq_mx_linear_act_codes(const void* a, int M, int K, const void* w, int N, const void* bias, int act, int gated, void* y, long ldy, int dtype,
+                           const void* residual, long ldr, void* pre, long ldpre, void* stream) {
+    int rc;
+    if ((rc = check_product_act(M, N, K, w, bias, act, gated, y, ldy, dtype, residual, ldr, pre, ldpre)) || (rc = check_mx(a, M, K))) return rc;
+    if (M == 0) return MQ_OK;
+    MxGemm g = product_act(M, K, w, N, bias, act, y, ldy, dtype, residual, ldr, pre, ldpre);
+    return run_act(g, gated, a, (hipStream_t)stream);
+}
+
+size_t mq_act_grad_workspace_bytes(int M, int N, int gated) { return M <= 0 || N <= 0 ? 0 : up256(act_grad_workspace_bytes(M, N, gated)); }
+
+int mq_act_grad(const void* dy, int M, int N, long lddy, const void* pre, long ldpre, int act, int gated, void* da, long ldda, int dtype, float* dbias, void* ws,
+                size_t ws_bytes, void* stream) {
+    if (!type_ok(dtype) || act <= MQ_ACT_NONE || act > MQ_ACT_SILU) return MQ_ERR_BAD_ARG;
+    if (M < 0 || M > (1 << 28) || N <= 0 || N > (1 << 22) || (gated && N % 2 != 0)) return MQ_ERR_BAD_SHAPE;
+    const int outs = gated ? N / 2 : N;
+    int rc;
+    if ((rc = check_matrix(dy, M, lddy, outs)) || (rc = check_matrix(pre, M, ldpre, N)) || (rc = check_matrix(da, M, ldda, N))) return rc;
+    if (!aligned(dbias, 4)) return MQ_ERR_BAD_ARG;
+    if (dbias) {
+        const size_t need = mq_act_grad_workspace_bytes(M, N, gated);
+        if (need > 0 && (!ws || !aligned(ws, 256))) return MQ_ERR_BAD_ARG;
+        if (ws_bytes < need) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    }
+    if (M > 0 && !(itself_or_apart(da, ldda, pre, ldpre, N, M) && (gated ? apart(da, ldda, N, dy, lddy, outs, M) : itself_or_apart(da, ldda, dy, lddy, N, M))))
+        return MQ_ERR_BAD_ARG;
+    ActGrad a = {};
+    a.dy = (const uint16_t*)dy, a.lddy = lddy, a.pre = (const uint16_t*)pre, a.ldpre = ldpre, a.M = M, a.N = N, a.act = act, a.gated = gated != 0;
+    a.da = (uint16_t*)da, a.ldda = ldda, a.dtype = dtype, a.dbias = dbias, a.partial = (float*)ws;
+    return launch_act_grad(a, (hipStream_t)stream);
+}
+
+int mq_mx_experts_column_top(const void* mx, int experts, int N, int K, uint8_t* top, void* stream) {
+    int rc;
+    if (experts <= 0 || experts > 4096 || N <= 0 || N % 32 != 0 || (long)N * experts > 1 << 28) return MQ_ERR_BAD_SHAPE;
+    if ((rc = check_mx(mx, N * experts, K))) return rc;
+    if (!top) return MQ_ERR_BAD_ARG;
+    return launch_mx_experts_column_top(mx, experts, N, K, top, (hipStream_t)stream);
+}
+
+size_t mq_mx_linear_grouped_workspace_bytes(int M, int N, int K, int experts) {
+    return M <= 0 || N <= 0 || K <= 0 || K % 32 != 0 || experts <= 0 ? 0 : up256(mx_experts_workspace_bytes(M, N, K, experts));
+}
+
+int mq_mx_linear_grouped(const void* x, int M, int K, long ldx, const void* w, int N, int experts, const int* offsets, const void* bias, int act, int gated,
+                         void* y, long ldy, int dtype, void* pre, long ldpre, void* ws, size_t ws_bytes, void* stream) {
+    if (!type_ok(dtype)) return MQ_ERR_BAD_ARG;
+    if (M < 0) return MQ_ERR_BAD_SHAPE;
+    int rc;
+    if ((rc = check_experts(w, N, K, experts, offsets, M)) || (rc = check_matrix(x, M, ldx, K))) return rc;
+    if (gated && N % 64 != 0) return MQ_ERR_BAD_SHAPE;
+    const int outs = gated ? N / 2 : N;
+    if ((rc = check_matrix(y, M, ldy, outs)) || (rc = check_act(M, N, act, gated, y, ldy, nullptr, pre, ldpre))) return rc;
+    if (!aligned(bias, 2)) return MQ_ERR_BAD_ARG;
+    if (gated && !gate_fits(N, K)) return MQ_ERR_BAD_SHAPE;
+    if (M == 0) return MQ_OK;
+    if (!apart(x, ldx, K, y, ldy, outs, M) || (pre && !apart(x, ldx, K, pre, ldpre, N, M))) return MQ_ERR_BAD_ARG;
+    const size_t need = mq_mx_linear_grouped_workspace_bytes(M, N, K, experts);
+    if (need > 0 && (!ws || !aligned(ws, 256))) return MQ_ERR_BAD_ARG;
+    if (ws_bytes < need) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    MxGemm g = product_act(M, K, w, N, bias, act, y, ldy, dtype, nullptr, 0, pre, ldpre);
+    g.w.scales = g.w.codes + (size_t)experts * g.w.groups * g.w.kc * 1024;
+    g.offsets = offsets, g.experts = experts;
+    return launch_mx_experts(g, gated, x, ldx, ws, (hipStream_t)stream);
+}
+
+size_t mq_mx_linear_grouped_grad_workspace_bytes(int M, int experts) { return M <= 0 || experts <= 0 ? 0 : up256(mx_experts_grad_workspace_bytes(M, experts)); }
+
+int mq_mx_linear_grouped_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, int experts, const int* offsets, void* dx,
+                              long lddx, int dtype, void* ws, size_t ws_bytes, void* stream) {
+    if (!type_ok(dtype) || !top) return MQ_ERR_BAD_ARG;
+    if (M < 0) return MQ_ERR_BAD_SHAPE;
+    int rc;
+    if ((rc = check_experts(w, N, K, experts, offsets, M)) || (rc = check_matrix(dy, M, lddy, N)) || (rc = check_matrix(dx, M, lddx, K))) return rc;
+    if (M == 0) return MQ_OK;
+    if (!ws || !aligned(ws, 256)) return MQ_ERR_BAD_ARG;
+    if (ws_bytes < mq_mx_linear_grouped_grad_workspace_bytes(M, experts)) return MQ_ERR_WORKSPACE_TOO_SMALL;
+    if (!apart(dx, lddx, K, dy, lddy, N, M)) return MQ_ERR_BAD_ARG;
+    return launch_mx_experts_grad(dy, M, N, lddy, w, top, K, experts, offsets, dx, lddx, dtype, ws, (hipStream_t)stream);
 }
 
 }  // extern "C"

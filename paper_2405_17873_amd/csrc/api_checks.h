@@ -33,4 +33,30 @@ inline int check_mx(const void* p, int rows, int K) {
     return MQ_OK;
 }
 
+inline int check_product(int M, int N, int K, const void* w, const void* bias, const void* y, long ldy, int dtype, const void* residual, long ldr) {
+    if (!type_ok(dtype)) return MQ_ERR_BAD_ARG;
+    if (M < 0 || N <= 0 || N > (1 << 22)) return MQ_ERR_BAD_SHAPE;
+    int rc;
+    if ((rc = check_mx(w, N, K))) return rc;
+    if (!aligned(bias, 2)) return MQ_ERR_BAD_ARG;
+    if ((rc = check_matrix(y, M, ldy, N))) return rc;
+    if (residual && (rc = check_matrix(residual, M, ldr, N))) return rc;
+    return MQ_OK;
+}
+
+inline MxGemm product(int M, int K, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual, long ldr) {
+    MxGemm g = {};
+    g.w = mx_view(w, N, K);
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.bias = (const uint16_t*)bias;
+    g.y = (uint16_t*)y;
+    g.ldy = ldy;
+    g.res = (const uint16_t*)residual;
+    g.ldr = ldr;
+    g.dtype = dtype;
+    return g;
+}
+
 }  // namespace mq

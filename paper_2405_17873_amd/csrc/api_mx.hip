@@ -5,31 +5,6 @@
 
 namespace mq {
 
-static int check_product(int M, int N, int K, const void* w, const void* bias, const void* y, long ldy, int dtype, const void* residual, long ldr) {
-    if (!type_ok(dtype)) return MQ_ERR_BAD_ARG;
-    if (M < 0 || N <= 0 || N > (1 << 22)) return MQ_ERR_BAD_SHAPE;
-    int rc;
-    if ((rc = check_mx(w, N, K))) return rc;
-    if (!aligned(bias, 2)) return MQ_ERR_BAD_ARG;
-    if ((rc = check_matrix(y, M, ldy, N))) return rc;
-    if (residual && (rc = check_matrix(residual, M, ldr, N))) return rc;
-    return MQ_OK;
-}
-
-static MxGemm product(int M, int K, const void* w, int N, const void* bias, void* y, long ldy, int dtype, const void* residual, long ldr) {
-    MxGemm g = {};
-    g.w = mx_view(w, N, K);
-    g.M = M;
-    g.N = N;
-    g.K = K;
-    g.bias = (const uint16_t*)bias;
-    g.y = (uint16_t*)y;
-    g.ldy = ldy;
-    g.res = (const uint16_t*)residual;
-    g.ldr = ldr;
-    g.dtype = dtype;
-    return g;
-}
 static int run(MxGemm& g, const void* a, hipStream_t st) {
     g.a = mx_view(a, g.M, g.K);
     return mx_rows_takes(g.M, g.N) ? launch_mx_rows(g, nullptr, 0, st) : launch_mx_gemm(g, st);

@@ -153,6 +153,10 @@ inline int allow_lds(PerDevice& prepared, const void* kernel, int bytes) {
     });
 }
 
+// What else a kernel of the product does: an activation on the sums (g.act, which may be none), and the sums themselves to g.pre if asked for; a gate: the columns of Y are
+// half those of the weights, the first half's sums times the activation of the second's; rows sorted by expert, the tiles by a plan made on the GPU.
+enum { MX_ACT = 1, MX_GATED = 2, MX_EXPERTS = 4 };
+
 // ---- launchers (arguments are checked by the entry points) ----
 struct MxGemm {
     MxView a, w;  // activations [M,K], weights [N,K]
@@ -163,19 +167,72 @@ struct MxGemm {
     const uint16_t* res;
     long ldr;
     int dtype;
+    // with an activation
+    int act;
+    uint16_t* pre;  // the sums, nullable
+    long ldpre;
+    // by expert: w is the first expert's
+    const struct MxRowPlan* plan;
+    const int* offsets;  // [experts + 1]
+    int experts;
 };
+// Row tiles of a product by expert, made on the GPU from the experts' offsets: a tile starts at row `start` and writes rows first .. end - 1 of what it covers.
+struct MxPlanTile {
+    int expert, start, first, end;
+};
+struct MxRowPlan {
+    uint32_t tiles, pad[3];
+    MxPlanTile tile[1];
+};
+// Entries of a row plan, the same for all lanes.
+typedef const __attribute__((address_space(4))) int const_int;
+__device__ __forceinline__ uint32_t mx_plan_tiles(const MxRowPlan* p) { return __builtin_amdgcn_readfirstlane(*(const_int*)(uintptr_t)p); }
+__device__ __forceinline__ MxPlanTile mx_plan_tile(const MxRowPlan* p, int i) {
+    const const_int* t = (const_int*)(uintptr_t)(p->tile + i);
+    return MxPlanTile{__builtin_amdgcn_readfirstlane(t[0]), __builtin_amdgcn_readfirstlane(t[1]), __builtin_amdgcn_readfirstlane(t[2]),
+                      __builtin_amdgcn_readfirstlane(t[3])};
+}
+// Most tiles of at least 32 rows that a plan can have: whole ones, and for each expert with rows one that is not whole and one more where tiles start with whole
+// groups of 32 rows and its first row is inside one.
+inline long mx_plan_bound(long M, int experts, int tile_rows) { return M / tile_rows + 2 * (M < experts ? M : experts); }
+inline size_t mx_plan_bytes(long M, int experts, int tile_rows) { return (sizeof(MxRowPlan) + mx_plan_bound(M, experts, tile_rows) * sizeof(MxPlanTile) + 255) / 256 * 256; }
+// Tiles of tile_rows rows; whole_groups: that start with a whole group of 32.
+int launch_mx_plan(const int* offsets, int experts, int M, int tile_rows, bool whole_groups, MxRowPlan* plan, hipStream_t st);
 int launch_mx_quantize(const void* x, int M, int K, long ldx, int dtype, void* mx, hipStream_t st);
 int launch_mx_dequantize(const void* mx, int M, int K, int dtype, void* y, long ldy, hipStream_t st);
 int launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int M, int K, void* mx, hipStream_t st);
 int launch_mx_unpack(const void* mx, int M, int K, uint8_t* codes, uint8_t* scales, hipStream_t st);
+int launch_mx_experts_column_top(const void* mx, int experts, int N, int K, uint8_t* top, hipStream_t st);
 int launch_mx_column_top(const void* mx, int rows, int K, uint8_t* top, hipStream_t st);
 int launch_mx_gemm(const MxGemm& g, hipStream_t st);
+int launch_mx_gemm_act(const MxGemm& g, bool gated, hipStream_t st);
 int launch_mx_rows(const MxGemm& g, const void* x, long ldx, hipStream_t st);  // x: 16-bit activations, or null: g.a
+int launch_mx_rows_act(const MxGemm& g, bool gated, const void* x, long ldx, hipStream_t st);
+int launch_mx_experts(const MxGemm& g, bool gated, const void* x, long ldx, void* ws, hipStream_t st);
+size_t mx_experts_workspace_bytes(long M, long N, long K, int experts);
 bool mx_rows_takes(int M, int N);
 bool mx_rows_quantizes(int M, int N, int K);
+int launch_mx_experts_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, int experts, const int* offsets, void* dx, long lddx,
+                           int dtype, void* ws, hipStream_t st);
+size_t mx_experts_grad_workspace_bytes(long M, int experts);
 int launch_mx_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* ws,
                    hipStream_t st);
 size_t mx_grad_workspace_bytes(long M, long N, long K);
+struct ActGrad {
+    const uint16_t* dy;  // [M, O], O = N, gated N / 2
+    long lddy;
+    const uint16_t* pre;  // [M, N]
+    long ldpre;
+    int M, N, act;
+    bool gated;
+    uint16_t* da;
+    long ldda;
+    int dtype;
+    float* dbias;    // nullable
+    float* partial;  // workspace
+};
+int launch_act_grad(const ActGrad& a, hipStream_t st);
+size_t act_grad_workspace_bytes(long M, long N, bool gated);
 
 struct NormArgs {
     const uint16_t* x;

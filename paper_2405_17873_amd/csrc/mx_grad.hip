@@ -24,6 +24,7 @@ struct MxGrad {
     uint16_t* dx;
     long lddx;
     bool wide;  // rows of dY start on 16-byte boundaries
+    const MxRowPlan* plan;  // by expert: w and top are the first expert's
 };
 
 // What is added to the scale bytes of a block column with the largest scale `top`, and taken back at the end.  fp16: 6 units of the largest are 49152.
@@ -110,7 +111,7 @@ struct GradPlan {
 // three units then.
 // Measured (bfloat16): 8192 x 8192 x 8192 1030 to 1045 us, 1.06 PFLOP/s (a library product of 16-bit matrices reaches 1.37), on zeros 870: a fifth is power.  With
 // no loads from memory 790 us.  A unit (32 MFMAs, 1024 cycles) keeps LDS busy for about as long: loads write 41 KB, widened weights 32, reads fetch 73.
-template <int DT, int TM, int NW, int S>
+template <int DT, int TM, int NW, int S, bool EXPERTS>
 __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, const GradWork work) {
     using P = GradPlan<TM, NW, S>;
     constexpr int TK = P::TK;
@@ -118,12 +119,26 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5;
     // whole tiles: neighbouring tiles of one row strip run on one XCD
-    const bool whole = blockIdx.x < work.whole;
-    const uint32_t xcd = blockIdx.x & 7, more = work.whole & 7;
-    const uint32_t tile_v = whole ? xcd * (work.whole >> 3) + (xcd < more ? xcd : more) + (blockIdx.x >> 3) : work.whole + (blockIdx.x - work.whole) / work.parts;
+    const uint32_t undivided = EXPERTS ? mx_plan_tiles(g.plan) * work.col_tiles : work.whole;
+    const bool whole = EXPERTS || blockIdx.x < work.whole;
+    const uint32_t xcd = blockIdx.x & 7, more = undivided & 7;
+    // (by expert, the launch has as many workgroups as there can be tiles)
+    if (EXPERTS && (blockIdx.x >> 3) >= (undivided >> 3) + (xcd < more ? 1u : 0u)) return;
+    const uint32_t tile_v = whole ? xcd * (undivided >> 3) + (xcd < more ? xcd : more) + (blockIdx.x >> 3) : work.whole + (blockIdx.x - work.whole) / work.parts;
     const uint32_t tile = __builtin_amdgcn_readfirstlane(tile_v);  // (divisions are done in vector registers)
     const uint32_t part = whole ? 0 : (blockIdx.x - work.whole) % work.parts, parts = whole ? 1 : work.parts;
-    const long m0 = (long)(tile / work.col_tiles) * (TM * 32);
+    const uint32_t tile_row = __builtin_amdgcn_readfirstlane(tile / work.col_tiles);
+    long m0 = (long)tile_row * (TM * 32);
+    int rows_end = g.M;
+    const uint8_t *codes = g.w.codes, *scales = g.w.scales, *top = g.top;
+    if constexpr (EXPERTS) {
+        const MxPlanTile t = mx_plan_tile(g.plan, (int)tile_row);
+        m0 = t.start;
+        rows_end = t.end;
+        codes += (long)t.expert * g.w.groups * g.w.kc * 1024;
+        scales += (long)t.expert * g.w.groups * g.w.kq * 256;
+        top += (long)t.expert * (g.K >> 5);
+    }
     const int b0 = __builtin_amdgcn_readfirstlane((int)(tile % work.col_tiles) * TK);  // first block column: half of a scale column
     const int kc = g.w.kc, kq = g.w.kq, blocks = g.K >> 5;
     const int g0 = __builtin_amdgcn_readfirstlane((int)((long)g.w.groups * part / parts)), g1 = __builtin_amdgcn_readfirstlane((int)((long)g.w.groups * (part + 1) / parts));
@@ -131,11 +146,11 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
     const uint32_t base = (uint32_t)(uintptr_t)lds + wv * P::WAVE;
     constexpr int OOB = 0x7FFFF000;
 
-    const long rows = g.M - m0 < TM * 32 ? g.M - m0 : TM * 32;
+    const long rows = rows_end - m0 < TM * 32 ? rows_end - m0 : TM * 32;
     const int n_end = g.N < g1 * 32 ? g.N : g1 * 32;
     const int4s rd = make_rsrc(g.dy + m0 * g.lddy, (uint32_t)(((rows - 1) * g.lddy + g.N) * 2));
-    const int4s rc = make_rsrc(g.w.codes, (uint32_t)((long)g1 * kc * 1024));
-    const int4s rs = make_rsrc(g.w.scales, (uint32_t)((long)g1 * kq * 256));
+    const int4s rc = make_rsrc(codes, (uint32_t)((long)g1 * kc * 1024));
+    const int4s rs = make_rsrc(scales, (uint32_t)((long)g1 * kq * 256));
     // dY: a load takes 16 rows x 64 bytes; piece p of row r lies at p ^ turned(r)
     const int piece = (lane & 3) ^ mx_turned(lane >> 2);
     const int v_dy = (int)((long)(lane >> 2) * g.lddy * 2) + piece * 16;
@@ -169,7 +184,7 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
     // widening: the lane has row wn (of 16) of block wb; its four pieces of eight columns lie at p ^ turned(wn)
     const int wn = lane & 15, wb = lane >> 4;
     const int b_mine = b0 + wb < blocks ? b0 + wb : blocks - 1;
-    const int shift = mx_grad_shift<DT>((int)g.top[b_mine]), sbit = 8 * ((b_mine >> 1) & 3);
+    const int shift = mx_grad_shift<DT>((int)top[b_mine]), sbit = 8 * ((b_mine >> 1) & 3);
     const uint32_t a_code = base + P::DY + wb * 512 + wn * 16, a_scale = base + P::DY + P::CODES + (b_mine & 1) * 128 + wn * 4;
     const uint32_t a_wide = base + S * P::SLOT;
     uint32_t a_write[4], a_read[2];
@@ -265,7 +280,7 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
     const uint32_t join = (uint32_t)(uintptr_t)lds;
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
-        if (m0 + m * 32 >= g.M) break;
+        if (m0 + m * 32 >= rows_end) break;
         if (m) __syncthreads();
 #pragma unroll
         for (int k = 0; k < TK; ++k)
@@ -280,7 +295,7 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
             const int row = v / (TK * 4), c = v % (TK * 4);
             const long mm = m0 + m * 32 + row;
             const int k = b0 * 32 + c * 8;
-            if (v < VECS && mm < g.M && k < g.K) {
+            if (v < VECS && mm < rows_end && k < g.K) {
                 float4v a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
 #pragma unroll
                 for (int w = 0; w < NW; ++w) {
@@ -289,7 +304,7 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
                     b += *(const lds_float4v*)(uintptr_t)(at + 16);
                 }
                 if (whole) {
-                    store8_16(g.dx + mm * g.lddx + k, mx_grad_result<DT>(a, b, (int)g.top[k >> 5]), 8);
+                    store8_16(g.dx + mm * g.lddx + k, mx_grad_result<DT>(a, b, (int)top[k >> 5]), 8);
                 } else {
                     float* out = work.partial + ((long)(blockIdx.x - work.whole) * (TM * 32) + m * 32 + row) * (TK * 32) + c * 8;
                     *(float4v*)out = a;
@@ -320,13 +335,24 @@ __global__ __launch_bounds__(256) void mx_grad_join_kernel(const MxGrad g, const
 }
 
 // Any alignment of dY's rows, any N, weights of any size: 64 x 64 results per workgroup, operands through registers.
-template <int DT>
+template <int DT, bool EXPERTS>
 __global__ __launch_bounds__(256) void mx_grad_any_kernel(const MxGrad g) {
     constexpr int BM = 64, BK = 64, BN = 64;
     __shared__ __attribute__((aligned(16))) uint8_t wt[BN * BK * 2];
     __shared__ __attribute__((aligned(16))) uint8_t dt[BM * BN * 2];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const long m0 = (long)blockIdx.x * BM;
+    long m0 = (long)blockIdx.x * BM;
+    int rows_end = g.M;
+    const uint8_t *codes = g.w.codes, *scales = g.w.scales, *top = g.top;
+    if constexpr (EXPERTS) {
+        if (blockIdx.x >= mx_plan_tiles(g.plan)) return;
+        const MxPlanTile t = mx_plan_tile(g.plan, (int)blockIdx.x);
+        m0 = t.start;
+        rows_end = t.end;
+        codes += (long)t.expert * g.w.groups * g.w.kc * 1024;
+        scales += (long)t.expert * g.w.groups * g.w.kq * 256;
+        top += (long)t.expert * (g.K >> 5);
+    }
     const int c = blockIdx.y, k0 = c * BK;
     const int wm = wv & 1, wk = wv >> 1;
     float16v acc = {};
@@ -338,10 +364,10 @@ __global__ __launch_bounds__(256) void mx_grad_any_kernel(const MxGrad g) {
             uint32_t s = 0, t = 0;
             if (n0 / 32 + grp < g.w.groups) {
                 const long G = n0 / 32 + grp;
-                v = *(const uint4v*)(g.w.codes + (G * g.w.kc + c) * 1024 + L * 16);
-                s = g.w.scales[(G * g.w.kq + (c >> 2)) * 256 + L * 4 + (c & 3)];
+                v = *(const uint4v*)(codes + (G * g.w.kc + c) * 1024 + L * 16);
+                s = scales[(G * g.w.kq + (c >> 2)) * 256 + L * 4 + (c & 3)];
                 const int b = c * 2 + kb;
-                t = b * 32 < g.K ? g.top[b] : 0;
+                t = b * 32 < g.K ? top[b] : 0;
             }
             const float sc = mx_grad_scale(s, mx_grad_shift<DT>((int)t));
 #pragma unroll
@@ -352,7 +378,7 @@ __global__ __launch_bounds__(256) void mx_grad_any_kernel(const MxGrad g) {
             const int t = i * 256 + tid, r = t >> 3, p = t & 7;
             const int n = n0 + p * 8;
             uint4v v = {0, 0, 0, 0};
-            if (m0 + r < g.M && n < g.N) v = load8_16(g.dy + (m0 + r) * g.lddy + n, g.N - n);
+            if (m0 + r < rows_end && n < g.N) v = load8_16(g.dy + (m0 + r) * g.lddy + n, g.N - n);
             *(uint4v*)(dt + r * (BN * 2) + ((p ^ (r & 7)) << 4)) = v;
         }
         __syncthreads();
@@ -374,8 +400,8 @@ __global__ __launch_bounds__(256) void mx_grad_any_kernel(const MxGrad g) {
     }
     const long m = m0 + wm * 32 + (lane & 31);
     const int kcol = k0 + wk * 32, h = lane >> 5;
-    if (kcol >= g.K || m >= g.M) return;
-    const int back = -mx_grad_shift<DT>((int)g.top[kcol >> 5]);
+    if (kcol >= g.K || m >= rows_end) return;
+    const int back = -mx_grad_shift<DT>((int)top[kcol >> 5]);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int k = kcol + 8 * (i >> 2) + 4 * h + (i & 3);
@@ -444,7 +470,7 @@ template <int DT, int TM, int NW, int S>
 static int run_mx_grad(const MxGrad& g, const GradForm& f, float* ws, hipStream_t st) {
     using P = GradPlan<TM, NW, S>;
     static_assert(P::BYTES <= 160 * 1024, "LDS of a compute unit");
-    auto kernel = mx_grad_kernel<DT, TM, NW, S>;
+    auto kernel = mx_grad_kernel<DT, TM, NW, S, false>;
     static PerDevice prepared;
     if (const int rc = allow_lds(prepared, (const void*)kernel, P::BYTES)) return rc;
     GradWork w;
@@ -474,7 +500,7 @@ static int choose_mx_grad(MxGrad g, float* ws, hipStream_t st) {
         g.dy = to, g.lddy = g.N = ld, g.wide = true;
     }
     if (!g.wide || g.N % 8 != 0 || !small || g.lddy >= (1 << 22)) {
-        mx_grad_any_kernel<DT><<<dim3((unsigned)((g.M + 63L) / 64), (unsigned)g.w.kc), 256, 0, st>>>(g);
+        mx_grad_any_kernel<DT, false><<<dim3((unsigned)((g.M + 63L) / 64), (unsigned)g.w.kc), 256, 0, st>>>(g);
         MQ_HIP_CHECK_LAUNCH();
         return MQ_OK;
     }
@@ -484,7 +510,7 @@ static int choose_mx_grad(MxGrad g, float* ws, hipStream_t st) {
 
 int launch_mx_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* ws,
                    hipStream_t st) {
-    MxGrad g;
+    MxGrad g = {};
     g.dy = (const uint16_t*)dy;
     g.lddy = M > 1 ? lddy : N;
     g.w = mx_view(w, N, K);
@@ -496,6 +522,53 @@ int launch_mx_grad(const void* dy, int M, int N, long lddy, const void* w, const
     g.lddx = lddx;
     g.wide = (M == 1 || g.lddy % 8 == 0) && (uintptr_t)dy % 16 == 0;
     return dtype == MQ_F16 ? choose_mx_grad<MQ_F16>(g, (float*)ws, st) : choose_mx_grad<MQ_BF16>(g, (float*)ws, st);
+}
+
+// By expert: a plan of row tiles that start at the experts' first rows, and a workgroup for every tile that there can be.  Tiles of 32, 64 or 128 rows by the
+// average number of an expert's rows.
+size_t mx_experts_grad_workspace_bytes(long M, int experts) { return mx_plan_bytes(M, experts, 32); }
+
+template <int DT, int TM, int NW, int S>
+static int run_mx_experts_grad(const MxGrad& g, int experts, hipStream_t st) {
+    using P = GradPlan<TM, NW, S>;
+    auto kernel = mx_grad_kernel<DT, TM, NW, S, true>;
+    static PerDevice prepared;
+    if (const int rc = allow_lds(prepared, (const void*)kernel, P::BYTES)) return rc;
+    GradWork w = {};
+    w.col_tiles = (uint32_t)((g.K / 32 + 3) / 4);
+    w.parts = 1;
+    kernel<<<(unsigned)((mx_plan_bound(g.M, experts, TM * 32) * w.col_tiles + 7) / 8 * 8), NW * 64, P::BYTES, st>>>(g, w);
+    MQ_HIP_CHECK_LAUNCH();
+    return MQ_OK;
+}
+template <int DT>
+static int choose_mx_experts_grad(const MxGrad& g, int experts, const int* offsets, hipStream_t st) {
+    const bool any = !g.wide || g.lddy >= (1 << 22) || (long)g.w.groups * g.w.kc * 1024 >= (1L << 31);
+    const int rows = any ? 64 : g.M <= 32L * experts ? 32 : g.M <= 64L * experts ? 64 : 128;
+    if (const int rc = launch_mx_plan(offsets, experts, g.M, rows, false, (MxRowPlan*)g.plan, st)) return rc;
+    if (any) {
+        mx_grad_any_kernel<DT, true><<<dim3((unsigned)mx_plan_bound(g.M, experts, rows), (unsigned)g.w.kc), 256, 0, st>>>(g);
+        MQ_HIP_CHECK_LAUNCH();
+        return MQ_OK;
+    }
+    return rows == 32 ? run_mx_experts_grad<DT, 1, 8, 3>(g, experts, st) : rows == 64 ? run_mx_experts_grad<DT, 2, 4, 5>(g, experts, st) : run_mx_experts_grad<DT, 4, 4, 3>(g, experts, st);
+}
+int launch_mx_experts_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, int experts, const int* offsets, void* dx, long lddx,
+                           int dtype, void* ws, hipStream_t st) {
+    MxGrad g = {};
+    g.dy = (const uint16_t*)dy;
+    g.lddy = M > 1 ? lddy : N;
+    g.w = mx_view(w, N, K);
+    g.w.scales = g.w.codes + (size_t)experts * g.w.groups * g.w.kc * 1024;
+    g.top = top;
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.dx = (uint16_t*)dx;
+    g.lddx = lddx;
+    g.wide = (M == 1 || g.lddy % 8 == 0) && (uintptr_t)dy % 16 == 0;
+    g.plan = (const MxRowPlan*)ws;
+    return dtype == MQ_F16 ? choose_mx_experts_grad<MQ_F16>(g, experts, offsets, st) : choose_mx_experts_grad<MQ_BF16>(g, experts, offsets, st);
 }
 
 }  // namespace mq

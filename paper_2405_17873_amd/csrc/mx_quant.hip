@@ -150,6 +150,8 @@ int launch_mx_unpack(const void* mx, int M, int K, uint8_t* codes, uint8_t* scal
 // top[b] = largest scale byte below 255 of block column b (0 if there is none).  A workgroup takes the eight block columns of a scale word column.
 __global__ __launch_bounds__(256) void mx_column_top_kernel(const uint8_t* scales, int groups, int kq, int blocks, uint8_t* top) {
     const int q = blockIdx.x, lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
+    scales += (long)blockIdx.y * groups * kq * 256;  // (of several matrices, one behind the other)
+    top += (long)blockIdx.y * blocks;
     uint32_t best[4] = {0, 0, 0, 0};
     for (int g = sub; g < groups; g += 4) {
         const uint32_t w = *(const uint32_t*)(scales + ((long)g * kq + q) * 256 + lane * 4);
@@ -175,6 +177,13 @@ __global__ __launch_bounds__(256) void mx_column_top_kernel(const uint8_t* scale
 int launch_mx_column_top(const void* mx, int rows, int K, uint8_t* top, hipStream_t st) {
     const MxView v = mx_view(mx, rows, K);
     mx_column_top_kernel<<<v.kq, 256, 0, st>>>(v.scales, v.groups, v.kq, K / 32, top);
+    MQ_HIP_CHECK_LAUNCH();
+    return MQ_OK;
+}
+
+int launch_mx_experts_column_top(const void* mx, int experts, int N, int K, uint8_t* top, hipStream_t st) {
+    const MxView v = mx_view(mx, (long)experts * N, K);
+    mx_column_top_kernel<<<dim3(v.kq, experts), 256, 0, st>>>(v.scales, v.groups / experts, v.kq, K / 32, top);
     MQ_HIP_CHECK_LAUNCH();
     return MQ_OK;
 }
