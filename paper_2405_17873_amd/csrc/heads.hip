@@ -1,10 +1,13 @@
 // Norm of every query and key head and its rotation by position, in one pass, and the gradient of both.
 //
-// A head is held by L lanes with NU units of eight values each (L NU of them, D / 8 used): a unit is four pairs, whose values lie together (interleaved) or
-// R / 2 apart, or, past the R values that turn, eight values.  Both values of a pair are in one lane, and a lane's pairs are the same in every head
-// of a row, so that an angle's sine and cosine are computed once for the heads that a wave takes of a row.
+// A head is held by L lanes (a power of two; D / 8 of them used) with a unit of eight values each: four pairs, whose values lie together (interleaved) or R / 2
+// apart, or, past the R values that turn, eight values.  Both values of a pair are in one lane, and a lane's pairs are the same in every head of a row, so that an
+// angle's sine and cosine are computed once for the heads that a wave takes of a row.  Waves walk over the rows; what depends on the lane alone stays in registers.
 //   y = T(x r w), r = 1 / sqrt(mean x^2 + eps), T the rotation of pair p by angle position[axis p] f_p
 //   g = T^-1 dy, dw = sum g x r, dx = r (g w - x r^2 mean(g w x))
+// Bound by memory.  us a call among others (bfloat16): forward 32768 x 40 heads of 64, three axes 63 (5.3 TB/s), 4096 x 40 of 128 14.6, gradient 98 and 25, 4 of it joining
+// the sums.  (Lanes with three or five units each, so that none is idle with heads of 96 or 80, needed 200 registers and more: 2964 x 32 heads of 80 50; sine and cosine
+// as polynomials, weights and table once per row 90 where the first takes 63.)
 // Angles: f / (2 pi) is a 64-bit fraction of a turn; its product with a position, modulo one turn, is exact integer arithmetic however far the position is.
 #include "lane_sum.h"
 #include "mx_common.h"
@@ -13,295 +16,327 @@ namespace mq {
 
 typedef uint2v uint2v_half __attribute__((aligned(2)));
 
-struct HeadUnit {
-    float re[4], im[4];
+struct HeadUnit {  // (vectors: arrays of floats that are read in other pairs than they were written in went through LDS, 8 -> 20 us of 2964 x 32 heads of 80)
+    float4v re, im;
 };
 
-// Sine and cosine of a 32-bit fraction of a turn: a quarter turn around zero is left after the quadrant, and the Taylor series to x^9 and x^8 are good to
-// 2 10^-9 and 3 10^-8 there.
-__device__ __forceinline__ void turn_sincos(uint32_t t, float& s, float& c) {
-    const uint32_t q = (t + 0x20000000u) >> 30;
-    const float x = (float)(int32_t)(t - (q << 30)) * 1.4629180792671596e-9f, z = x * x;  // 2 pi / 2^32
-    const float ps = x + x * z * (-1.6666667e-1f + z * (8.3333333e-3f + z * (-1.9841270e-4f + z * 2.7557319e-6f)));
-    const float pc = 1.0f + z * (-0.5f + z * (4.1666668e-2f + z * (-1.3888889e-3f + z * 2.4801587e-5f)));
-    s = q & 1 ? pc : ps;
-    c = q & 1 ? ps : pc;
-    if (q & 2) s = -s;
-    if ((q + 1) & 2) c = -c;
-}
-
-__device__ __forceinline__ float head_param(const void* p, int dtype, int i) {
-    if (dtype == MQ_F32) return ((const float*)p)[i];
-    const uint16_t b = ((const uint16_t*)p)[i];
-    return dtype == MQ_F16 ? T16<MQ_F16>::up(b) : T16<MQ_BF16>::up(b);
-}
-
-// What a lane knows of its units: where their two runs of four values start in a head, whether they exist, and whether they turn.
-template <int L, int NU>
-struct HeadLane {
-    int lo[NU], hi[NU], first[NU];
-    bool in[NU], turns[NU];
-    __device__ __forceinline__ HeadLane(const HeadArgs& a, int sub, bool interleaved) {
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int u = i * L + sub;
-            in[i] = u * 8 < a.D;
-            turns[i] = u * 4 < a.pairs;
-            first[i] = u * 4;
-            const bool split = turns[i] && !interleaved;
-            lo[i] = in[i] ? (split ? u * 4 : u * 8) : 0;
-            hi[i] = in[i] ? (split ? a.pairs + u * 4 : u * 8 + 4) : 4;
-        }
+// A row's positions: lane k has that of axis k modulo 4 (or the last).  (Scalar loads would be waited for one by one, some 0.5 us each.)
+struct HeadPosition {
+    uint32_t low, high;
+    __device__ __forceinline__ void load(const HeadArgs& a, long row) {
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.pos + row * a.ldpos * a.pos_bytes), 0, a.axes * a.pos_bytes, 0x00020000);
+        const int k = threadIdx.x & 3, at = (k < a.axes ? k : a.axes - 1) * a.pos_bytes;
+        low = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+        high = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, at + a.pos_bytes - 4, 0, 0);
     }
 };
-
-template <int L, int NU>
-__device__ __forceinline__ void head_angles(const HeadArgs& a, const HeadLane<L, NU>& lane, long row, float (*sn)[4], float (*cs)[4]) {
-    uint2v pos[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        pos[i] = uint2v{0, 0};
-        if (i < a.axes) {
-            const long at = row * a.ldpos + i;
-            if (a.pos_bytes == 8) {
-                const unsigned long long v = ((const unsigned long long*)a.pos)[at];
-                pos[i] = uint2v{(uint32_t)v, (uint32_t)(v >> 32)};
-            } else {
-                const int v = ((const int*)a.pos)[at];
-                pos[i] = uint2v{(uint32_t)v, (uint32_t)(v >> 31)};
-            }
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < NU; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            sn[i][j] = 0.0f, cs[i][j] = 1.0f;
-            if (lane.turns[i]) {
-                const uint4v f = a.table[lane.first[i] + j];  // a turn's fraction (low, high), axis
-                uint32_t p0 = pos[0][0], p1 = pos[0][1];
-#pragma unroll
-                for (int k = 1; k < 4; ++k) p0 = f[2] == (uint32_t)k ? pos[k][0] : p0, p1 = f[2] == (uint32_t)k ? pos[k][1] : p1;
-                turn_sincos(f[1] * p0 + __umulhi(f[0], p0) + f[0] * p1, sn[i][j], cs[i][j]);
-            }
-        }
-}
-
-// Four raw pairs of a unit into numbers.
-template <int DT, bool INTER>
-__device__ __forceinline__ HeadUnit head_widen(uint2v lo, uint2v hi) {
-    HeadUnit u;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float a = T16<DT>::up((uint16_t)(lo[j >> 1] >> (16 * (j & 1)))), b = T16<DT>::up((uint16_t)(hi[j >> 1] >> (16 * (j & 1))));
-        if (!INTER) {
-            u.re[j] = a, u.im[j] = b;
-        } else if (j & 1) {
-            u.im[j >> 1] = a, u.im[2 + (j >> 1)] = b;
-        } else {
-            u.re[j >> 1] = a, u.re[2 + (j >> 1)] = b;
-        }
-    }
-    return u;
-}
-template <int DT, bool INTER>
-__device__ __forceinline__ void head_pack(const HeadUnit& u, uint2v& lo, uint2v& hi) {
-    if (INTER) {
-        lo = uint2v{T16<DT>::pack(u.re[0], u.im[0]), T16<DT>::pack(u.re[1], u.im[1])};
-        hi = uint2v{T16<DT>::pack(u.re[2], u.im[2]), T16<DT>::pack(u.re[3], u.im[3])};
-    } else {
-        lo = uint2v{T16<DT>::pack(u.re[0], u.re[1]), T16<DT>::pack(u.re[2], u.re[3])};
-        hi = uint2v{T16<DT>::pack(u.im[0], u.im[1]), T16<DT>::pack(u.im[2], u.im[3])};
-    }
-}
-template <bool INTER>
-__device__ __forceinline__ int head_value(int j, bool im) {  // which of a unit's eight values (0 .. 3 the first run) pair j's is
-    return INTER ? 2 * j + im : 4 * im + j;
-}
-
-template <int DT, int L, int NU, bool INTER>
-__device__ __forceinline__ void head_weights(const HeadArgs& a, const HeadLane<L, NU>& lane, const void* p, HeadUnit* w) {
-#pragma unroll
-    for (int i = 0; i < NU; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = head_value<INTER>(j, false), m = head_value<INTER>(j, true);
-            w[i].re[j] = p && lane.in[i] ? head_param(p, a.param_dtype, (r < 4 ? lane.lo[i] : lane.hi[i] - 4) + r) : 1.0f;
-            w[i].im[j] = p && lane.in[i] ? head_param(p, a.param_dtype, (m < 4 ? lane.lo[i] : lane.hi[i] - 4) + m) : 1.0f;
-        }
-}
-__device__ __forceinline__ HeadUnit head_either(bool first, const HeadUnit& a, const HeadUnit& b) {
-    HeadUnit u;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) u.re[j] = first ? a.re[j] : b.re[j], u.im[j] = first ? a.im[j] : b.im[j];
-    return u;
-}
-// (What does not turn stays as it is, infinities included.)
-__device__ __forceinline__ HeadUnit head_turn(const HeadUnit& u, const float* s, const float* c, bool turns, float way) {
-    HeadUnit o;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float sj = s[j] * way;
-        o.re[j] = turns ? u.re[j] * c[j] - u.im[j] * sj : u.re[j];
-        o.im[j] = turns ? u.re[j] * sj + u.im[j] * c[j] : u.im[j];
-    }
-    return o;
-}
-
-// A wave takes a chunk of the heads of one row, 64 / L of them at a time and U such turns in flight.
-template <int DT, int L, int NU, bool INTER>
-__global__ __launch_bounds__(256) void heads_kernel(const HeadArgs a) {
-    constexpr int G = 64 / L, U = NU == 1 ? 4 : NU == 3 ? 2 : 1;
-    const int ln = threadIdx.x & 63, grp = ln / L;
-    const uint32_t task = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    uint32_t row_v, chunk_v;
-    a.chunks.divmod(task, row_v, chunk_v);
-    const int row = __builtin_amdgcn_readfirstlane((int)row_v), chunk = __builtin_amdgcn_readfirstlane((int)chunk_v);
-    if (row >= a.M) return;
-    const int H = a.q + a.k, h0 = chunk * a.per_chunk, h1 = h0 + a.per_chunk < H ? h0 + a.per_chunk : H;
-    const HeadLane<L, NU> lane(a, ln % L, INTER);
-    const uint16_t* x = a.x + row * a.ldx;
-    uint16_t* y = a.y + row * a.ldy;
-    float sn[NU][4], cs[NU][4];
-    HeadUnit wq[NU], wk[NU];
-    const float mean = 1.0f / (float)a.D;
-    for (int base = h0; base < h1; base += G * U) {
-        uint2v lo[U][NU], hi[U][NU];
-#pragma unroll
-        for (int t = 0; t < U; ++t) {
-            const int h = base + t * G + grp;
-#pragma unroll
-            for (int i = 0; i < NU; ++i) {
-                const bool in = h < h1 && lane.in[i];
-                const uint16_t* p = x + (in ? h * a.D : 0);
-                lo[t][i] = in ? *(const uint2v_half*)(p + lane.lo[i]) : uint2v{0, 0};
-                hi[t][i] = in ? *(const uint2v_half*)(p + lane.hi[i]) : uint2v{0, 0};
-            }
-        }
-        if (base == h0) {
-            head_angles<L, NU>(a, lane, row, sn, cs);
-            head_weights<DT, L, NU, INTER>(a, lane, a.qw, wq);
-            head_weights<DT, L, NU, INTER>(a, lane, a.kw, wk);
-        }
-#pragma unroll
-        for (int t = 0; t < U; ++t) {
-            const int h = base + t * G + grp;
-            HeadUnit u[NU];
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NU; ++i) {
-                u[i] = head_widen<DT, INTER>(lo[t][i], hi[t][i]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum += u[i].re[j] * u[i].re[j] + u[i].im[j] * u[i].im[j];
-            }
-            if (a.norm) {
-                const float r = rsqrtf(lane_sum<L>(sum) * mean + a.eps);
-#pragma unroll
-                for (int i = 0; i < NU; ++i) {
-                    const HeadUnit w = head_either(h < a.q, wq[i], wk[i]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) u[i].re[j] = u[i].re[j] * r * w.re[j], u[i].im[j] = u[i].im[j] * r * w.im[j];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < NU; ++i) {
-                uint2v o0, o1;
-                head_pack<DT, INTER>(head_turn(u[i], sn[i], cs[i], lane.turns[i], 1.0f), o0, o1);
-                if (h < h1 && lane.in[i]) {
-                    *(uint2v_half*)(y + h * a.D + lane.lo[i]) = o0;
-                    *(uint2v_half*)(y + h * a.D + lane.hi[i]) = o1;
-                }
-            }
-        }
-    }
-}
-
-// The gradient: waves walk over the rows (and chunks of their heads), and hold the sums for the weights of their units; a workgroup joins those of its
-// lanes and waves in a fixed order, and a second kernel those of the workgroups.
-template <int DT, int L, int NU, bool INTER>
-__global__ __launch_bounds__(256) void heads_grad_kernel(const HeadArgs a) {
-    constexpr int G = 64 / L, U = NU == 1 ? 2 : 1;
-    __shared__ float join[4 * 64 * NU * 8];
-    const int ln = threadIdx.x & 63, wv = threadIdx.x >> 6, grp = ln / L, sub = ln % L;
-    const HeadLane<L, NU> lane(a, sub, INTER);
-    HeadUnit wq[NU], wk[NU], sums[2][NU];
-    head_weights<DT, L, NU, INTER>(a, lane, a.qw, wq);
-    head_weights<DT, L, NU, INTER>(a, lane, a.kw, wk);
-#pragma unroll
-    for (int i = 0; i < NU; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sums[0][i].re[j] = sums[0][i].im[j] = sums[1][i].re[j] = sums[1][i].im[j] = 0.0f;
-    const int H = a.q + a.k;
-    const float mean = 1.0f / (float)a.D;
-    for (uint32_t task_v = blockIdx.x * 4 + wv; task_v < a.tasks; task_v += gridDim.x * 4) {
-        const uint32_t task = __builtin_amdgcn_readfirstlane(task_v);
+// Where a wave is in its tasks: chunks of the heads of a row, `step` heads at a time.
+struct HeadWalk {
+    uint32_t task;
+    int row, base, end;
+    __device__ __forceinline__ void enter(const HeadArgs& a) {
         uint32_t row_v, chunk_v;
         a.chunks.divmod(task, row_v, chunk_v);
-        const int row = __builtin_amdgcn_readfirstlane((int)row_v), chunk = __builtin_amdgcn_readfirstlane((int)chunk_v);
-        const int h0 = chunk * a.per_chunk, h1 = h0 + a.per_chunk < H ? h0 + a.per_chunk : H;
-        const uint16_t *x = a.x + row * a.ldx, *dy = a.dy + row * a.lddy;
-        uint16_t* dx = a.dx + row * a.lddx;
-        float sn[NU][4], cs[NU][4];
-        for (int base = h0; base < h1; base += G * U) {
-            uint2v lo[U][NU], hi[U][NU], dlo[U][NU], dhi[U][NU];
+        const int chunk = __builtin_amdgcn_readfirstlane((int)chunk_v), H = a.q + a.k;
+        row = __builtin_amdgcn_readfirstlane((int)row_v);
+        base = chunk * a.per_chunk;
+        end = base + a.per_chunk < H ? base + a.per_chunk : H;
+    }
+    __device__ __forceinline__ HeadWalk(const HeadArgs& a, uint32_t first) : task(__builtin_amdgcn_readfirstlane(first)), row(0), base(0), end(0) {
+        if (more(a)) enter(a);
+    }
+    __device__ __forceinline__ bool more(const HeadArgs& a) const { return task < a.tasks; }
+    __device__ __forceinline__ void next(const HeadArgs& a, int step, uint32_t waves) {
+        base += step;
+        if (base < end) return;
+        task += waves;
+        if (more(a)) enter(a);
+    }
+};
+
+// What a lane knows of its unit: where its two runs of four values start in a head, whether it exists, and whether it turns; its pairs' fractions and axes.
+template <int L, bool INTER>
+struct HeadLane {
+    int first, lo, hi;
+    bool in, turns;
+    uint4v f0, f1, axis;
+    __device__ __forceinline__ HeadLane(const HeadArgs& a, int sub) {
+        first = sub * 4;
+        in = sub * 8 < a.D;
+        turns = sub * 4 < a.pairs;
+        const bool split = turns && !INTER;
+        lo = in ? (split ? sub * 4 : sub * 8) : 0;
+        hi = in ? (split ? a.pairs + sub * 4 : sub * 8 + 4) : 4;
+    }
+    __device__ __forceinline__ void load_table(const HeadArgs& a) {  // (zeros where nothing turns)
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)a.table, 0, a.pairs * 16, 0x00020000);
 #pragma unroll
-            for (int t = 0; t < U; ++t) {
-                const int h = base + t * G + grp;
+        for (int j = 0; j < 4; ++j) {
+            const uint4v f = __builtin_amdgcn_raw_buffer_load_b128(r, (first + j) * 16, 0, 0);  // a turn's fraction (low, high), axis
+            f0[j] = f[0], f1[j] = f[1], axis[j] = f[2];
+        }
+    }
+    // Sines and cosines of a row: those of a lane that does not turn are 0 and 1.  The hardware's functions take turns (measured: off by at most
+    // 2 10^-7 over a turn).
+    __device__ __forceinline__ void angles(const HeadArgs& a, const HeadPosition& p, float4v& s, float4v& c) const {
+        if (a.axes == 0) {
 #pragma unroll
-                for (int i = 0; i < NU; ++i) {
-                    const bool in = h < h1 && lane.in[i];
-                    const int at = in ? h * a.D : 0;
-                    dlo[t][i] = in ? *(const uint2v_half*)(dy + at + lane.lo[i]) : uint2v{0, 0};
-                    dhi[t][i] = in ? *(const uint2v_half*)(dy + at + lane.hi[i]) : uint2v{0, 0};
-                    lo[t][i] = in && a.norm ? *(const uint2v_half*)(x + at + lane.lo[i]) : uint2v{0, 0};
-                    hi[t][i] = in && a.norm ? *(const uint2v_half*)(x + at + lane.hi[i]) : uint2v{0, 0};
+            for (int j = 0; j < 4; ++j) s[j] = 0.0f, c[j] = 1.0f;
+            return;
+        }
+        uint4v t, p0, p1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            p0[k] = (uint32_t)__builtin_amdgcn_readlane((int)p.low, k);
+            p1[k] = a.pos_bytes == 8 ? (uint32_t)__builtin_amdgcn_readlane((int)p.high, k) : (uint32_t)((int)p0[k] >> 31);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t q0 = p0[0], q1 = p1[0];
+            if (a.axes > 1) {
+#pragma unroll
+                for (int k = 1; k < 4; ++k) q0 = axis[j] == (uint32_t)k ? p0[k] : q0, q1 = axis[j] == (uint32_t)k ? p1[k] : q1;
+            }
+            t[j] = f1[j] * q0 + __umulhi(f0[j], q0);
+            t[j] += a.pos_bytes == 8 ? f0[j] * q1 : q1 ? 0u - f0[j] : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float turn = (float)(int32_t)t[j] * 2.3283064e-10f;  // 2^-32
+            s[j] = __builtin_amdgcn_sinf(turn);
+            c[j] = __builtin_amdgcn_cosf(turn);
+        }
+    }
+    // Four raw pairs into numbers, and back.
+    template <int DT>
+    static __device__ __forceinline__ HeadUnit widen(uint4v v) {
+        HeadUnit u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = INTER ? 2 * j : j, m = INTER ? 2 * j + 1 : 4 + j;
+            u.re[j] = T16<DT>::up((uint16_t)(v[r >> 1] >> (16 * (r & 1))));
+            u.im[j] = T16<DT>::up((uint16_t)(v[m >> 1] >> (16 * (m & 1))));
+        }
+        return u;
+    }
+    template <int DT>
+    static __device__ __forceinline__ uint4v pack(const HeadUnit& u) {
+        if (INTER)
+            return uint4v{T16<DT>::pack(u.re[0], u.im[0]), T16<DT>::pack(u.re[1], u.im[1]), T16<DT>::pack(u.re[2], u.im[2]), T16<DT>::pack(u.re[3], u.im[3])};
+        return uint4v{T16<DT>::pack(u.re[0], u.re[1]), T16<DT>::pack(u.re[2], u.re[3]), T16<DT>::pack(u.im[0], u.im[1]), T16<DT>::pack(u.im[2], u.im[3])};
+    }
+    __device__ __forceinline__ uint4v load(const uint16_t* head) const {
+        if (INTER) return *(const uint4v_any*)(head + lo);
+        const uint2v a = *(const uint2v_half*)(head + lo), b = *(const uint2v_half*)(head + hi);
+        return uint4v{a[0], a[1], b[0], b[1]};
+    }
+    __device__ __forceinline__ void store(uint16_t* head, uint4v v) const {
+        if (INTER) {
+            *(uint4v_any*)(head + lo) = v;
+        } else {
+            *(uint2v_half*)(head + lo) = uint2v{v[0], v[1]};
+            *(uint2v_half*)(head + hi) = uint2v{v[2], v[3]};
+        }
+    }
+    // Both weights; their loads come first.
+    __device__ __forceinline__ void weights(const HeadArgs& a, HeadUnit& q, HeadUnit& k) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q.re[j] = q.im[j] = k.re[j] = k.im[j] = 1.0f;
+        if (!in) return;
+        if (a.param_dtype == MQ_F32) {
+            typedef float4v float4v_any __attribute__((aligned(4)));
+            const float *of_q = (const float*)(a.qw ? a.qw : a.kw), *of_k = (const float*)(a.kw ? a.kw : a.qw);
+            if (!of_q) return;
+            const float4v f[2][2] = {{*(const float4v_any*)(of_q + lo), *(const float4v_any*)(of_q + hi)}, {*(const float4v_any*)(of_k + lo), *(const float4v_any*)(of_k + hi)}};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = INTER ? 2 * j : j, m = INTER ? 2 * j + 1 : 4 + j;
+                if (a.qw) q.re[j] = f[0][r >> 2][r & 3], q.im[j] = f[0][m >> 2][m & 3];
+                if (a.kw) k.re[j] = f[1][r >> 2][r & 3], k.im[j] = f[1][m >> 2][m & 3];
+            }
+            return;
+        }
+        const uint16_t *of_q = (const uint16_t*)(a.qw ? a.qw : a.kw), *of_k = (const uint16_t*)(a.kw ? a.kw : a.qw);
+        if (!of_q) return;
+        const uint4v rq = load(of_q), rk = load(of_k);
+        const bool half = a.param_dtype == MQ_F16;
+        if (a.qw) q = half ? widen<MQ_F16>(rq) : widen<MQ_BF16>(rq);
+        if (a.kw) k = half ? widen<MQ_F16>(rk) : widen<MQ_BF16>(rk);
+    }
+};
+
+// A row of heads.  WIDE (rows on 16-byte boundaries): through a buffer resource, so that a lane without a head needs no branch and the number of stores ahead of
+// a load is known, which then need not be waited for.
+template <bool WIDE, int L, bool INTER>
+struct HeadRow {
+    uint16_t* p;
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ __forceinline__ HeadRow(const uint16_t* row, int values) : p((uint16_t*)row) {
+        if constexpr (WIDE) rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, values * 2, 0x00020000);
+    }
+    __device__ __forceinline__ uint4v load(const HeadLane<L, INTER>& lane, int at, bool in) const {
+        if constexpr (!WIDE) return in ? lane.load(p + at) : uint4v{0, 0, 0, 0};
+        const int lo = in ? (at + lane.lo) * 2 : -16;
+        if constexpr (INTER) return __builtin_amdgcn_raw_buffer_load_b128(rsrc, lo, 0, 0);
+        const auto a = __builtin_amdgcn_raw_buffer_load_b64(rsrc, lo, 0, 0), b = __builtin_amdgcn_raw_buffer_load_b64(rsrc, in ? (at + lane.hi) * 2 : -16, 0, 0);
+        return uint4v{(uint32_t)a[0], (uint32_t)a[1], (uint32_t)b[0], (uint32_t)b[1]};
+    }
+    __device__ __forceinline__ void store(const HeadLane<L, INTER>& lane, int at, bool in, uint4v v) const {
+        if constexpr (!WIDE) {
+            if (in) lane.store(p + at, v);
+        } else {
+            const int lo = in ? (at + lane.lo) * 2 : -16;
+            if constexpr (INTER) {
+                __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, lo, 0, WRITE_THROUGH);
+            } else {
+                __builtin_amdgcn_raw_buffer_store_b64(uint2v{v[0], v[1]}, rsrc, lo, 0, WRITE_THROUGH);
+                __builtin_amdgcn_raw_buffer_store_b64(uint2v{v[2], v[3]}, rsrc, in ? (at + lane.hi) * 2 : -16, 0, WRITE_THROUGH);
+            }
+        }
+    }
+};
+__device__ __forceinline__ float either(bool first, float a, float b) { return first ? a : b; }
+
+// A wave takes chunks of the heads of a row: 64 / L of them at a time, U such turns in flight.
+template <int DT, int L, bool INTER, bool WIDE>
+__global__ __launch_bounds__(256) void heads_kernel(const HeadArgs a) {
+    using Row = HeadRow<WIDE, L, INTER>;
+    constexpr int G = 64 / L, U = 4;
+    const int values = (a.q + a.k) * a.D;
+    const int ln = threadIdx.x & 63, grp = ln / L;
+    const float mean = 1.0f / (float)a.D;
+    HeadLane<L, INTER> lane(a, ln % L);
+    const uint32_t waves = gridDim.x * 4;
+    HeadWalk at(a, blockIdx.x * 4 + (threadIdx.x >> 6));
+    uint4v ahead[U];
+    HeadPosition pos;
+    auto fetch = [&]() {  // the heads at `at`
+        const Row x(a.x + at.row * a.ldx, values);
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            const int h = at.base + t * G + grp;
+            ahead[t] = x.load(lane, h * a.D, h < at.end && lane.in);
+        }
+        pos.load(a, at.row);
+    };
+    if (at.more(a)) fetch();
+    lane.load_table(a);
+    HeadUnit wq, wk;
+    lane.weights(a, wq, wk);
+    int row = -1;
+    float4v s, c;
+    while (at.more(a)) {
+        uint4v v[U];
+#pragma unroll
+        for (int t = 0; t < U; ++t) v[t] = ahead[t];
+        if (at.row != row) lane.angles(a, pos, s, c);
+        row = at.row;
+        const int base = at.base, h1 = at.end;
+        const Row y(a.y + row * a.ldy, values);
+        at.next(a, G * U, waves);
+        if (at.more(a)) fetch();
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            const int h = base + t * G + grp;
+            HeadUnit u = lane.template widen<DT>(v[t]);
+            if (a.norm) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum += u.re[j] * u.re[j] + u.im[j] * u.im[j];
+                const float r = rsqrtf(lane_sum<L>(sum) * mean + a.eps);
+                const bool is_q = h < a.q;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u.re[j] *= r * either(is_q, wq.re[j], wk.re[j]), u.im[j] *= r * either(is_q, wq.im[j], wk.im[j]);
+            }
+            HeadUnit o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {  // (what does not turn stays as it is, infinities included)
+                o.re[j] = lane.turns ? u.re[j] * c[j] - u.im[j] * s[j] : u.re[j];
+                o.im[j] = lane.turns ? u.re[j] * s[j] + u.im[j] * c[j] : u.im[j];
+            }
+            y.store(lane, h * a.D, h < h1 && lane.in, lane.template pack<DT>(o));
+        }
+    }
+}
+
+// The gradient: lanes also hold the sums for the weights of their units; a workgroup joins those of its lanes and waves in a fixed order, and a second kernel
+// those of the workgroups.
+constexpr int HG_WAVES = 8;
+template <int DT, int L, bool INTER, bool WIDE>
+__global__ __launch_bounds__(HG_WAVES * 64) void heads_grad_kernel(const HeadArgs a) {
+    using Row = HeadRow<WIDE, L, INTER>;
+    constexpr int G = 64 / L, U = 2;
+    const int values = (a.q + a.k) * a.D;
+    __shared__ float join[HG_WAVES * 64 * 8];
+    const int ln = threadIdx.x & 63, wv = threadIdx.x >> 6, grp = ln / L, sub = ln % L;
+    HeadLane<L, INTER> lane(a, sub);
+    HeadUnit sums[2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[0].re[j] = sums[0].im[j] = sums[1].re[j] = sums[1].im[j] = 0.0f;
+    const float mean = 1.0f / (float)a.D;
+    const uint32_t waves = gridDim.x * HG_WAVES;
+    HeadWalk at(a, blockIdx.x * HG_WAVES + wv);
+    uint4v x_ahead[U], d_ahead[U];
+    HeadPosition pos;
+    auto fetch = [&]() {
+        const Row x(a.norm ? a.x + at.row * a.ldx : nullptr, values), dy(a.dy + at.row * a.lddy, values);
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            const int h = at.base + t * G + grp;
+            const bool in = h < at.end && lane.in;
+            d_ahead[t] = dy.load(lane, h * a.D, in);
+            x_ahead[t] = x.load(lane, h * a.D, in && a.norm);
+        }
+        pos.load(a, at.row);
+    };
+    if (at.more(a)) fetch();
+    lane.load_table(a);
+    HeadUnit wq, wk;
+    lane.weights(a, wq, wk);
+    int row = -1;
+    float4v s, c;
+    while (at.more(a)) {
+        uint4v xv[U], dv[U];
+#pragma unroll
+        for (int t = 0; t < U; ++t) xv[t] = x_ahead[t], dv[t] = d_ahead[t];
+        if (at.row != row) lane.angles(a, pos, s, c);
+        row = at.row;
+        const int base = at.base, h1 = at.end;
+        const Row dx(a.dx + row * a.lddx, values);
+        at.next(a, G * U, waves);
+        if (at.more(a)) fetch();
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            const int h = base + t * G + grp;
+            const bool is_q = h < a.q, live = h < h1;
+            const HeadUnit d = lane.template widen<DT>(dv[t]);
+            HeadUnit g;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g.re[j] = lane.turns ? d.re[j] * c[j] + d.im[j] * s[j] : d.re[j];
+                g.im[j] = lane.turns ? d.im[j] * c[j] - d.re[j] * s[j] : d.im[j];
+            }
+            if (a.norm) {
+                const HeadUnit v = lane.template widen<DT>(xv[t]);
+                float sq = 0.0f, dot = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sq += v.re[j] * v.re[j] + v.im[j] * v.im[j];
+                    dot += g.re[j] * either(is_q, wq.re[j], wk.re[j]) * v.re[j] + g.im[j] * either(is_q, wq.im[j], wk.im[j]) * v.im[j];
+                }
+                const float r = rsqrtf(lane_sum<L>(sq) * mean + a.eps), back = lane_sum<L>(dot) * mean * r * r;
+                // (of lanes that hold no head only zeros come: but 0 r is none where r is infinite, as without eps)
+                const float rl = live ? r : 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float dr = g.re[j] * v.re[j] * rl, di = g.im[j] * v.im[j] * rl;
+                    sums[0].re[j] += either(is_q, dr, 0.0f), sums[0].im[j] += either(is_q, di, 0.0f);
+                    sums[1].re[j] += either(is_q, 0.0f, dr), sums[1].im[j] += either(is_q, 0.0f, di);
+                    g.re[j] = r * (g.re[j] * either(is_q, wq.re[j], wk.re[j]) - v.re[j] * back);
+                    g.im[j] = r * (g.im[j] * either(is_q, wq.im[j], wk.im[j]) - v.im[j] * back);
                 }
             }
-            if (base == h0) head_angles<L, NU>(a, lane, row, sn, cs);
-#pragma unroll
-            for (int t = 0; t < U; ++t) {
-                const int h = base + t * G + grp;
-                const bool is_q = h < a.q, live = h < h1;
-                HeadUnit g[NU];
-#pragma unroll
-                for (int i = 0; i < NU; ++i) g[i] = head_turn(head_widen<DT, INTER>(dlo[t][i], dhi[t][i]), sn[i], cs[i], lane.turns[i], -1.0f);
-                if (a.norm) {
-                    HeadUnit v[NU];
-                    float sq = 0.0f, dot = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < NU; ++i) {
-                        v[i] = head_widen<DT, INTER>(lo[t][i], hi[t][i]);
-                        const HeadUnit w = head_either(is_q, wq[i], wk[i]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            sq += v[i].re[j] * v[i].re[j] + v[i].im[j] * v[i].im[j];
-                            dot += g[i].re[j] * w.re[j] * v[i].re[j] + g[i].im[j] * w.im[j] * v[i].im[j];
-                        }
-                    }
-                    const float r = rsqrtf(lane_sum<L>(sq) * mean + a.eps), back = lane_sum<L>(dot) * mean * r * r;
-#pragma unroll
-                    for (int i = 0; i < NU; ++i) {
-                        const HeadUnit w = head_either(is_q, wq[i], wk[i]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float dr = live ? g[i].re[j] * (v[i].re[j] * r) : 0.0f, di = live ? g[i].im[j] * (v[i].im[j] * r) : 0.0f;
-                            sums[0][i].re[j] += is_q ? dr : 0.0f, sums[0][i].im[j] += is_q ? di : 0.0f;
-                            sums[1][i].re[j] += is_q ? 0.0f : dr, sums[1][i].im[j] += is_q ? 0.0f : di;
-                            g[i].re[j] = r * (g[i].re[j] * w.re[j] - v[i].re[j] * back);
-                            g[i].im[j] = r * (g[i].im[j] * w.im[j] - v[i].im[j] * back);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < NU; ++i) {
-                    uint2v o0, o1;
-                    head_pack<DT, INTER>(g[i], o0, o1);
-                    if (live && lane.in[i]) {
-                        *(uint2v_half*)(dx + h * a.D + lane.lo[i]) = o0;
-                        *(uint2v_half*)(dx + h * a.D + lane.hi[i]) = o1;
-                    }
-                }
-            }
+            dx.store(lane, h * a.D, live && lane.in, lane.template pack<DT>(g));
         }
     }
     if (!a.partial) return;
@@ -309,48 +344,46 @@ __global__ __launch_bounds__(256) void heads_grad_kernel(const HeadArgs a) {
     for (int part = 0; part < 2; ++part) {
         if (part) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < NU; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float* p = join + (wv * G + grp) * (L * NU * 8) + (i * L + sub) * 8;
-                p[head_value<INTER>(j, false)] = sums[part][i].re[j];
-                p[head_value<INTER>(j, true)] = sums[part][i].im[j];
-            }
+        for (int j = 0; j < 4; ++j) join[threadIdx.x * 8 + j] = sums[part].re[j], join[threadIdx.x * 8 + 4 + j] = sums[part].im[j];
         __syncthreads();
-        for (int c = threadIdx.x; c < a.D; c += 256) {
-            float s = 0.0f;
-            for (int w = 0; w < 4 * G; ++w) s += join[w * (L * NU * 8) + c];
-            const int u = c >> 3, e = c & 7;
-            const int at = u * 4 < a.pairs && !INTER ? (e < 4 ? u * 4 + e : a.pairs + u * 4 + e - 4) : c;
-            a.partial[((long)blockIdx.x * 2 + part) * a.D + at] = s;
+        for (int c = threadIdx.x; c < a.D; c += HG_WAVES * 64) {
+            const int of = c >> 3, e = c & 7;  // lane of a head, value of its unit
+            float t = 0.0f;
+            for (int w = 0; w < HG_WAVES * G; ++w) t += join[(w * L + of) * 8 + e];
+            const bool turns = of * 4 < a.pairs;
+            const int at = INTER || !turns ? of * 8 + (INTER ? 2 * (e & 3) + (e >> 2) : e) : (e < 4 ? of * 4 + e : a.pairs + of * 4 + e - 4);
+            a.partial[((long)blockIdx.x * 2 + part) * a.D + at] = t;
         }
     }
 }
 
-// [parts][2 D] -> two vectors of D: 64 sums to a workgroup, each in four runs of parts.
+// [parts][2 D] -> two vectors of D: eight sums to a workgroup, each in 32 runs of parts.
 __global__ __launch_bounds__(256) void heads_join_kernel(const float* partial, int parts, int D, float* dq, float* dk) {
-    __shared__ float run[4][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+    __shared__ float run[32][8];
+    const int e = threadIdx.x & 7, c = blockIdx.x * 8 + e, slice = threadIdx.x >> 3;
     float s = 0.0f;
-    if (c < 2 * D) {
-#pragma unroll 8
-        for (int p = parts * slice / 4; p < parts * (slice + 1) / 4; ++p) s += partial[(long)p * 2 * D + c];
-    }
-    run[slice][threadIdx.x & 63] = s;
+#pragma unroll 4
+    for (int p = slice; p < parts; p += 32) s += partial[(long)p * 2 * D + c];
+    run[slice][e] = s;
     __syncthreads();
-    if (slice == 0 && c < 2 * D) {
-        s = (run[0][c & 63] + run[1][c & 63]) + (run[2][c & 63] + run[3][c & 63]);
+    if (slice == 0) {
+        s = 0.0f;
+        for (int i = 0; i < 32; ++i) s += run[i][e];
         float* out = c < D ? dq : dk;
         if (out) out[c < D ? c : c - D] = s;
     }
 }
 
 // Workgroups of the gradient, and so parts of its sums: at most as many as the chip holds at once.
-static long heads_grad_workgroups(long tasks) { return tasks <= 0 ? 0 : (tasks + 3) / 4 < 1024 ? (tasks + 3) / 4 : 1024; }
-// Waves for every row: as many as bring the launch to 2048 (eight per compute unit), but no part of a turn's heads.
+static long heads_grad_workgroups(long tasks) {
+    const long n = (tasks + HG_WAVES - 1) / HG_WAVES;
+    return n < 512 ? n : 512;
+}
+// Waves for every row: as many as bring the launch to 4096 (16 per compute unit), but no part of a turn's heads.  us, 2048 / 4096 / 8192 waves: forward 2964 x 32 heads
+// of 80 8.4 / 8.7 / 11.0, 4096 x 40 of 128 14.5 / 14.6 / 15.8, 32768 x 40 of 64 65 / 63 / 63; gradient 19.9 / 16.7 / 21.6, 24.8 / 24.9 / 26.0, 96 / 98 / 98.
 static void heads_chunks(HeadArgs& a, int L) {
     const int H = a.q + a.k, G = 64 / L, turns = (H + G - 1) / G;
-    long want = a.M > 0 ? (2048 + a.M - 1) / a.M : 1;
+    long want = a.M > 0 ? (4096 + a.M - 1) / a.M : 1;
     if (want > turns) want = turns;
     const int per = (int)((turns + want - 1) / want);
     a.per_chunk = per * G;
@@ -359,51 +392,39 @@ static void heads_chunks(HeadArgs& a, int L) {
     a.tasks = (uint32_t)((long)a.M * chunks);
 }
 
-template <int DT, int L, int NU>
+template <int DT, int L, bool INTER, bool WIDE>
 static int run_heads(HeadArgs& a, bool grad, hipStream_t st) {
     heads_chunks(a, L);
     if (!grad) {
-        const unsigned wgs = (unsigned)(((long)a.tasks + 3) / 4);
-        if (a.interleaved)
-            heads_kernel<DT, L, NU, true><<<wgs, 256, 0, st>>>(a);
-        else
-            heads_kernel<DT, L, NU, false><<<wgs, 256, 0, st>>>(a);
+        const long n = ((long)a.tasks + 3) / 4;
+        heads_kernel<DT, L, INTER, WIDE><<<(unsigned)(n < 1024 ? n : 1024), 256, 0, st>>>(a);
         MQ_HIP_CHECK_LAUNCH();
         return MQ_OK;
     }
     const long wgs = heads_grad_workgroups(a.tasks);
     if (!a.dq_weight && !a.dk_weight) a.partial = nullptr;
     if (wgs > 0) {
-        if (a.interleaved)
-            heads_grad_kernel<DT, L, NU, true><<<(unsigned)wgs, 256, 0, st>>>(a);
-        else
-            heads_grad_kernel<DT, L, NU, false><<<(unsigned)wgs, 256, 0, st>>>(a);
+        heads_grad_kernel<DT, L, INTER, WIDE><<<(unsigned)wgs, HG_WAVES * 64, 0, st>>>(a);
         MQ_HIP_CHECK_LAUNCH();
     }
     if (a.dq_weight || a.dk_weight) {
-        heads_join_kernel<<<(unsigned)((2 * a.D + 63) / 64), 256, 0, st>>>(a.partial, (int)wgs, a.D, a.dq_weight, a.dk_weight);
+        heads_join_kernel<<<(unsigned)(a.D / 4), 256, 0, st>>>(a.partial, (int)wgs, a.D, a.dq_weight, a.dk_weight);
         MQ_HIP_CHECK_LAUNCH();
     }
     return MQ_OK;
 }
-// Lanes and units for a head of n units of eight values: the fewest idle ones.
+template <int DT, int L>
+static int run_heads(HeadArgs& a, bool grad, hipStream_t st) {
+    auto wide = [&](const void* p, long ld) { return (uintptr_t)p % 16 == 0 && (a.M == 1 || ld % 8 == 0); };
+    const bool w = grad ? wide(a.dy, a.lddy) && wide(a.dx, a.lddx) && (!a.norm || wide(a.x, a.ldx)) : wide(a.x, a.ldx) && wide(a.y, a.ldy);
+    if (w) return a.interleaved ? run_heads<DT, L, true, true>(a, grad, st) : run_heads<DT, L, false, true>(a, grad, st);
+    return a.interleaved ? run_heads<DT, L, true, false>(a, grad, st) : run_heads<DT, L, false, false>(a, grad, st);
+}
 template <int DT>
 static int choose_heads(HeadArgs& a, bool grad, hipStream_t st) {
     const int n = a.D / 8;
-    if (n <= 1) return run_heads<DT, 1, 1>(a, grad, st);
-    if (n <= 2) return run_heads<DT, 2, 1>(a, grad, st);
-    if (n <= 3) return run_heads<DT, 1, 3>(a, grad, st);
-    if (n <= 4) return run_heads<DT, 4, 1>(a, grad, st);
-    if (n <= 5) return run_heads<DT, 1, 5>(a, grad, st);
-    if (n <= 6) return run_heads<DT, 2, 3>(a, grad, st);
-    if (n <= 8) return run_heads<DT, 8, 1>(a, grad, st);
-    if (n <= 10) return run_heads<DT, 2, 5>(a, grad, st);
-    if (n <= 12) return run_heads<DT, 4, 3>(a, grad, st);
-    if (n <= 16) return run_heads<DT, 16, 1>(a, grad, st);
-    if (n <= 20) return run_heads<DT, 4, 5>(a, grad, st);
-    if (n <= 24) return run_heads<DT, 8, 3>(a, grad, st);
-    if (n <= 32) return run_heads<DT, 32, 1>(a, grad, st);
-    return run_heads<DT, 64, 1>(a, grad, st);
+    return n <= 4 ? run_heads<DT, 4>(a, grad, st) : n <= 8 ? run_heads<DT, 8>(a, grad, st) : n <= 16 ? run_heads<DT, 16>(a, grad, st)
+           : n <= 32 ? run_heads<DT, 32>(a, grad, st) : run_heads<DT, 64>(a, grad, st);
 }
 
 size_t heads_grad_workspace_bytes(long M, int H, int D) {
