@@ -87,7 +87,9 @@ def _load_native():
             "mq_qlinear_w_only", "mq_qlinear_w8a8", "mq_qlinear_w4a8", "mq_qlinear_w2a8", "mq_quantize_weights", "mq_pack_weights",
             "mq_split_workspace_bytes", "mq_qlinear_a8_workspace_bytes", "mq_packed_bytes", "mq_mx_bytes", "mq_mx_quantize", "mq_mx_dequantize",
             "mq_mx_linear_workspace_bytes", "mq_mx_linear", "mq_mx_linear_codes", "mq_mx_linear_grad_workspace_bytes", "mq_mx_linear_grad",
-            "mq_layer_norm", "mq_layer_norm_mx", "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad")))
+            "mq_layer_norm", "mq_layer_norm_mx", "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad",
+            "mq_qk_norm_rope", "mq_qk_norm_rope_grad_workspace_bytes", "mq_qk_norm_rope_grad", "mq_mx_linear_act", "mq_act_grad_workspace_bytes", "mq_act_grad",
+            "mq_mx_linear_grouped_workspace_bytes", "mq_mx_linear_grouped", "mq_mx_linear_grouped_grad_workspace_bytes", "mq_mx_linear_grouped_grad")))
         _native = _mqhost
     return _native
 
@@ -1079,6 +1081,10 @@ def rotary(sections, theta: float = 10000.0, interleaved: bool = False, device=N
     return Rotary(torch.from_numpy(table).to(device), pairs, len(sections), bool(interleaved))
 
 
+def _rotary_parts(r: Optional[Rotary]):
+    return (None, 0, 0, False) if r is None else (r.table, r.pairs, r.axes, r.interleaved)
+
+
 def _head_args(x: torch.Tensor, q_heads: int, k_heads: int, q_weight, k_weight, rot: Optional[Rotary], positions, eps, norm: bool):
     """Arguments from the sizes to the positions, checked; what they point to has to live until the call."""
     M, cols = x.shape
@@ -1117,6 +1123,10 @@ def qk_norm_rope(x: torch.Tensor, q_heads: int, k_heads: int, q_weight: Optional
     """Norm of every query and key head, x w / sqrt(mean x^2 + eps), and its rotation by position.  x [M, (q_heads + k_heads) D] fp16/bf16: a row's
     query heads, then its key heads (of a stacked q, k, v the columns in front of the values: qkv[:, :n], with out the same to work in place).  q_weight, k_weight [D]
     in 16 bits or float32.  rotary: from rotary(); positions: int32 or int64 [M, axes], [M] for one axis.  norm=False: the rotation alone.  out may be x."""
+    if out is None:
+        r = (_native or _load_native()).qk_norm_rope(x, q_heads, k_heads, q_weight, k_weight, *_rotary_parts(rotary), positions, eps, norm)
+        if r is not None:
+            return _done(r, "mq_qk_norm_rope")
     _no_graph("qk_norm_rope", x, q_weight, k_weight)
     _matrix(x)
     _on_current(x.device)
@@ -1136,6 +1146,10 @@ def qk_norm_rope_grad(dy: torch.Tensor, x: Optional[torch.Tensor], q_heads: int,
                       norm: bool = True, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """(dx, dq_weight, dk_weight) of qk_norm_rope, x its input; the latter two float32 [D], sums over rows and heads, None without a norm (which needs no x
     either).  out may be dy or x."""
+    if out is None and ws is None and norm:
+        r = (_native or _load_native()).qk_norm_rope_grad(dy, x, q_heads, k_heads, q_weight, k_weight, *_rotary_parts(rotary), positions, eps, norm)
+        if r is not None:
+            return _done(r, "mq_qk_norm_rope_grad")
     _no_graph("qk_norm_rope_grad", dy)
     _matrix(dy)
     _on_current(dy.device)
@@ -1175,6 +1189,10 @@ def _mx_linear_act(x, w: MxTensor, bias, out, residual, ws, dtype, act, gated: b
     if act is None:
         raise ValueError("gated and want_pre go with an activation")
     code = _act_code(act, gated)
+    if out is None and ws is None and dtype is None and not packed:
+        r = (_native or _load_native()).mx_linear_act(x, w.data, w.rows, w.K, bias, residual, code, gated, want_pre)
+        if r is not None:
+            return _done(r, "mq_mx_linear_act")
     _no_graph("mx_linear", None if packed else x, bias, residual)
     if packed:
         M, K, device = x.rows, x.K, x.data.device
@@ -1216,6 +1234,10 @@ def act_grad(dy: torch.Tensor, pre: torch.Tensor, act: str, gated: bool = False,
     code = _act_code(act, gated)
     if not code:
         raise ValueError("act_grad is behind an activation")
+    if out is None and ws is None and want_dbias:
+        r = (_native or _load_native()).act_grad(dy, pre, code, gated)
+        if r is not None:
+            return _done(r, "mq_act_grad")
     _no_graph("act_grad", dy, pre)
     M, N = _matrix(pre).shape
     _on_current(pre.device)
@@ -1266,6 +1288,10 @@ def mx_linear_grouped(x: torch.Tensor, w: MxTensor, offsets: torch.Tensor, bias:
     code = _act_code(act, gated)
     if want_pre and act is None:
         raise ValueError("want_pre goes with an activation")
+    if out is None and ws is None and w.experts > 0 and w.rows % w.experts == 0:
+        r = (_native or _load_native()).mx_linear_grouped(x, w.data, w.rows // w.experts, w.K, w.experts, offsets, bias, code, gated, want_pre)
+        if r is not None:
+            return _done(r, "mq_mx_linear_grouped")
     _no_graph("mx_linear_grouped", x, bias)
     M, K = _matrix(x).shape
     device = x.device
@@ -1292,6 +1318,10 @@ def mx_linear_grouped_grad_workspace_bytes(M: int, experts: int) -> int:
 def mx_linear_grouped_grad(dy: torch.Tensor, w: MxTensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
                            ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dX[r] = dY[r] . W_e, the gradient of mx_linear_grouped with respect to its rows (the quantisation passed straight through).  out shares nothing with dy."""
+    if out is None and ws is None and w.top is not None and w.experts > 0 and w.rows % w.experts == 0:
+        r = (_native or _load_native()).mx_linear_grouped_grad(dy, w.data, w.rows // w.experts, w.K, w.experts, w.top, offsets)
+        if r is not None:
+            return _done(r, "mq_mx_linear_grouped_grad")
     _no_graph("mx_linear_grouped_grad", dy)
     M, N = _matrix(dy).shape
     _on_current(dy.device)

@@ -44,6 +44,16 @@ typedef int (*norm_mx_fn)(const void*, int, int, long, const void*, const void*,
 typedef int (*norm_grad_fn)(const void*, long, const void*, long, int, int, const void*, int, const float*, const float*, const void*, long, void*, long,
                             int, float*, float*, void*, size_t, void*);
 
+typedef int (*heads_fn)(const void*, int, int, int, int, long, const void*, const void*, int, float, int, const void*, int, int, const void*, int, int, long, void*,
+                        long, int, void*);
+typedef size_t (*heads_ws_fn)(int, int, int, int);
+typedef int (*heads_grad_fn)(const void*, long, const void*, int, int, int, int, long, const void*, const void*, int, float, int, const void*, int, int, const void*,
+                             int, int, long, void*, long, int, float*, float*, void*, size_t, void*);
+typedef int (*mx_act_fn)(const void*, int, int, long, const void*, int, const void*, int, int, void*, long, int, const void*, long, void*, long, void*, size_t, void*);
+typedef int (*act_grad_fn)(const void*, int, int, long, const void*, long, int, int, void*, long, int, float*, void*, size_t, void*);
+typedef int (*grouped_fn)(const void*, int, int, long, const void*, int, int, const int*, const void*, int, int, void*, long, int, void*, long, void*, size_t, void*);
+typedef int (*grouped_grad_fn)(const void*, int, int, long, const void*, const uint8_t*, int, int, const int*, void*, long, int, void*, size_t, void*);
+
 struct Entry {
     w_only_fn w_only;
     w8a8_fn w8a8;
@@ -65,6 +75,16 @@ struct Entry {
     norm_mx_fn norm_mx;
     mx_bytes_fn norm_grad_ws;
     norm_grad_fn norm_grad;
+    heads_fn heads;
+    heads_ws_fn heads_grad_ws;
+    heads_grad_fn heads_grad;
+    mx_act_fn mx_act;
+    mx_ws_fn act_grad_ws;
+    act_grad_fn act_grad;
+    heads_ws_fn grouped_ws;
+    grouped_fn grouped;
+    mx_bytes_fn grouped_grad_ws;
+    grouped_grad_fn grouped_grad;
 } entry;
 
 // An ordinary tensor on the GPU (torch.Tensor or Parameter itself), or nullptr.
@@ -564,6 +584,232 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
 }
 
+// ---- around the microscaled linears of a transformer block
+
+bool on_current(at::Device device) { return device.index() == c10::hip::getCurrentHIPStream().device_index(); }
+
+// (q_heads, k_heads, q_weight, k_weight, table, pairs, axes, interleaved, positions, eps, norm): what is the same for the heads' norm and its gradient
+struct Heads {
+    int q, k, D, param_type, pairs, axes, pos_bytes;
+    void *qw, *kw, *table, *pos;
+    bool interleaved, norm;
+    float eps;
+    long ldpos;
+};
+bool heads(PyObject* const* a, const Matrix& x, Heads& h) {
+    const at::Device device = x.t->device();
+    at::ScalarType tq = at::kFloat, tk = at::kFloat;
+    const at::Tensor *table = nullptr, *pos = nullptr;
+    if (!small_int(a[0], h.q) || !small_int(a[1], h.k) || h.q < 0 || h.k < 0 || h.q > 4096 || h.k > 4096 || h.q + h.k == 0 || x.cols % (h.q + h.k) != 0) return false;
+    h.D = x.cols / (h.q + h.k);
+    if (!vector(a[2], h.D, device, h.qw, &tq) || !vector(a[3], h.D, device, h.kw, &tk) || (h.qw && h.kw && tq != tk)) return false;
+    const at::ScalarType t = h.qw ? tq : tk;
+    h.param_type = t == at::kFloat ? 2 : dtype_of(t);
+    if (h.param_type < 0 || !flag(a[7], h.interleaved) || !PyFloat_CheckExact(a[9]) || !flag(a[10], h.norm) || (!h.norm && (h.qw || h.kw))) return false;
+    h.eps = (float)PyFloat_AS_DOUBLE(a[9]);
+    h.pairs = h.axes = 0, h.pos_bytes = 4, h.ldpos = 0;
+    if (!optional_ptr(a[4], h.table, &table) || !optional_ptr(a[8], h.pos, &pos) || !table != !pos) return false;
+    if (!table) return true;
+    if (!small_int(a[5], h.pairs) || !small_int(a[6], h.axes) || h.pairs <= 0 || h.axes < 1 || h.axes > 4) return false;
+    if (table->device() != device || table->scalar_type() != at::kInt || !table->is_contiguous() || table->numel() != (int64_t)h.pairs * 4) return false;
+    const bool line = pos->dim() == 1 && h.axes == 1;
+    if (pos->device() != device || !(line || (pos->dim() == 2 && pos->size(1) == h.axes)) || pos->size(0) != x.rows) return false;
+    if (pos->scalar_type() != at::kInt && pos->scalar_type() != at::kLong) return false;
+    if (!line && h.axes > 1 && pos->stride(1) != 1) return false;
+    h.pos_bytes = pos->scalar_type() == at::kInt ? 4 : 8;
+    h.ldpos = x.rows > 1 ? (long)pos->stride(0) : h.axes;
+    return h.ldpos >= h.axes;
+}
+
+// (x, heads ...) -> y, code or None
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix x;
+        Heads h;
+        if (n != 12 || !plain_calls() || !matrix(a[0], x) || !heads(a + 1, x, h) || !on_current(x.t->device()) || in_graph({a[0], a[3], a[4]})) return general();
+        at::Tensor y;
+        int rc;
+        {
+            Unlocked unlocked;
+            y = empty({x.rows, x.cols}, x.t->scalar_type(), x.t->device());
+            rc = entry.heads(x.p, x.rows, h.q, h.k, h.D, x.ld, h.qw, h.kw, h.param_type, h.eps, h.norm, h.table, h.pairs, h.interleaved, h.pos, h.pos_bytes, h.axes,
+                             h.ldpos, y.data_ptr(), x.cols, x.dtype, stream());
+        }
+        return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(std::move(y));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// (dy, x, heads ...) -> (dx, dq_weight, dk_weight), code or None; with a norm only
+PyObject* qk_norm_rope_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix dy, x;
+        Heads h;
+        if (n != 13 || !plain_calls() || !matrix(a[0], dy) || !matrix(a[1], x) || dy.rows != x.rows || dy.cols != x.cols || dy.dtype != x.dtype ||
+            dy.t->device() != x.t->device() || !heads(a + 2, x, h) || !h.norm || !on_current(x.t->device()) || in_graph({a[0]}))
+            return general();
+        const at::Device device = x.t->device();
+        at::Tensor dx, dq, dk, ws;
+        int rc;
+        {
+            Unlocked unlocked;
+            dx = empty({x.rows, x.cols}, x.t->scalar_type(), device);
+            dq = empty({h.D}, at::kFloat, device), dk = empty({h.D}, at::kFloat, device);
+            const size_t need = entry.heads_grad_ws(x.rows, h.q, h.k, h.D);
+            ws = workspace(need, device);
+            rc = entry.heads_grad(dy.p, dy.ld, x.p, x.rows, h.q, h.k, h.D, x.ld, h.qw, h.kw, h.param_type, h.eps, h.norm, h.table, h.pairs, h.interleaved, h.pos,
+                                  h.pos_bytes, h.axes, h.ldpos, dx.data_ptr(), x.cols, x.dtype, (float*)dq.data_ptr(), (float*)dk.data_ptr(), ws.data_ptr(), need,
+                                  stream());
+        }
+        return rc ? PyLong_FromLong(rc) : pair_or_more({dx, dq, dk});
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// (x, w, N, K, bias, residual, act, gated, want_pre) -> y or (y, pre), code or None
+PyObject* mx_linear_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix x, res;
+        int N, K, act;
+        void *w, *bias;
+        bool gated, want;
+        if (n != 9 || !plain_calls() || !matrix(a[0], x) || !small_int(a[2], N) || !small_int(a[3], K) || x.cols != K || !mx_data(a[1], N, K, w, x.t) ||
+            !small_int(a[6], act) || !flag(a[7], gated) || !flag(a[8], want) || (gated && (N % 64 != 0 || a[5] != Py_None)) || !on_current(x.t->device()) ||
+            in_graph({a[0], a[4], a[5]}))
+            return general();
+        const at::Device device = x.t->device();
+        at::ScalarType type = x.t->scalar_type();
+        if (!vector(a[4], N, device, bias, &type) || type != x.t->scalar_type() || !optional_matrix(a[5], x.rows, N, x.dtype, device, res)) return general();
+        const int outs = gated ? N / 2 : N;
+        at::Tensor y, pre, ws;
+        int rc;
+        {
+            Unlocked unlocked;
+            y = empty({x.rows, outs}, type, device);
+            if (want) pre = empty({x.rows, N}, type, device);
+            const size_t need = entry.mx_linear_ws(x.rows, N, K);
+            if (need) ws = workspace(need, device);
+            rc = entry.mx_act(x.p, x.rows, K, x.ld, w, N, bias, act, gated, y.data_ptr(), outs, x.dtype, res.p, res.ld, want ? pre.data_ptr() : nullptr, N,
+                              need ? ws.data_ptr() : nullptr, need, stream());
+        }
+        if (rc) return PyLong_FromLong(rc);
+        return want ? pair_or_more({y, pre}) : THPVariable_Wrap(std::move(y));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// (dy, pre, act, gated) -> (da, dbias), code or None
+PyObject* act_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix dy, pre;
+        int act;
+        bool gated;
+        if (n != 4 || !plain_calls() || !matrix(a[0], dy) || !matrix(a[1], pre) || !small_int(a[2], act) || !flag(a[3], gated) || (gated && pre.cols % 2 != 0) ||
+            dy.rows != pre.rows || dy.cols != (gated ? pre.cols / 2 : pre.cols) || dy.dtype != pre.dtype || dy.t->device() != pre.t->device() ||
+            !on_current(pre.t->device()) || in_graph({a[0], a[1]}))
+            return general();
+        const at::Device device = pre.t->device();
+        at::Tensor da, dbias, ws;
+        int rc;
+        {
+            Unlocked unlocked;
+            da = empty({pre.rows, pre.cols}, pre.t->scalar_type(), device);
+            dbias = empty({pre.cols}, at::kFloat, device);
+            const size_t need = entry.act_grad_ws(pre.rows, pre.cols, gated);
+            ws = workspace(need, device);
+            rc = entry.act_grad(dy.p, pre.rows, pre.cols, dy.ld, pre.p, pre.ld, act, gated, da.data_ptr(), pre.cols, pre.dtype, (float*)dbias.data_ptr(),
+                                ws.data_ptr(), need, stream());
+        }
+        return rc ? PyLong_FromLong(rc) : pair_or_more({da, dbias});
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// The experts' offsets, on the device of another operand.
+const int* offsets_of(PyObject* o, int experts, const at::Tensor* beside) {
+    const at::Tensor* t = gpu_tensor(o);
+    if (!t || experts <= 0 || t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) != (int64_t)experts + 1 || !t->is_contiguous() || t->device() != beside->device())
+        return nullptr;
+    return (const int*)t->data_ptr();
+}
+
+// (x, w, N, K, experts, offsets, bias, act, gated, want_pre) -> y or (y, pre), code or None
+PyObject* mx_linear_grouped(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix x;
+        int N, K, experts, act;
+        void *w, *bias = nullptr;
+        bool gated, want;
+        const int* offsets;
+        if (n != 10 || !plain_calls() || !matrix(a[0], x) || !small_int(a[2], N) || !small_int(a[3], K) || !small_int(a[4], experts) || x.cols != K || N <= 0 ||
+            N % 32 != 0 || experts <= 0 || (int64_t)N * experts > 1 << 28 || !mx_data(a[1], N * experts, K, w, x.t) || !(offsets = offsets_of(a[5], experts, x.t)) ||
+            !small_int(a[7], act) || !flag(a[8], gated) || !flag(a[9], want) || (gated && N % 64 != 0) || !on_current(x.t->device()) || in_graph({a[0], a[6]}))
+            return general();
+        const at::Device device = x.t->device();
+        const at::ScalarType type = x.t->scalar_type();
+        const at::Tensor* b = nullptr;
+        if (!optional_ptr(a[6], bias, &b)) return general();
+        if (b && (b->dim() != 2 || b->size(0) != experts || b->size(1) != N || !b->is_contiguous() || b->scalar_type() != type || b->device() != device)) return general();
+        const int outs = gated ? N / 2 : N;
+        at::Tensor y, pre, ws;
+        int rc;
+        {
+            Unlocked unlocked;
+            y = empty({x.rows, outs}, type, device);
+            if (want) pre = empty({x.rows, N}, type, device);
+            const size_t need = entry.grouped_ws(x.rows, N, K, experts);
+            if (need) ws = workspace(need, device);
+            rc = entry.grouped(x.p, x.rows, K, x.ld, w, N, experts, offsets, bias, act, gated, y.data_ptr(), outs, x.dtype, want ? pre.data_ptr() : nullptr, N,
+                               need ? ws.data_ptr() : nullptr, need, stream());
+        }
+        if (rc) return PyLong_FromLong(rc);
+        return want ? pair_or_more({y, pre}) : THPVariable_Wrap(std::move(y));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
+// (dy, w, N, K, experts, top, offsets) -> dx, code or None
+PyObject* mx_linear_grouped_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix dy;
+        int N, K, experts;
+        void* w;
+        const at::Tensor* top;
+        const int* offsets;
+        if (n != 7 || !plain_calls() || !matrix(a[0], dy) || !small_int(a[2], N) || !small_int(a[3], K) || !small_int(a[4], experts) || dy.cols != N ||
+            N % 32 != 0 || experts <= 0 || (int64_t)N * experts > 1 << 28 || !mx_data(a[1], N * experts, K, w, dy.t) || !(top = gpu_tensor(a[5])) ||
+            top->scalar_type() != at::kByte || !top->is_contiguous() || top->numel() != (int64_t)experts * (K / 32) || top->device() != dy.t->device() ||
+            !(offsets = offsets_of(a[6], experts, dy.t)) || !on_current(dy.t->device()) || in_graph({a[0]}))
+            return general();
+        const void* tp = top->data_ptr();
+        const at::Device device = dy.t->device();
+        at::Tensor dx, ws;
+        int rc;
+        {
+            Unlocked unlocked;
+            dx = empty({dy.rows, K}, dy.t->scalar_type(), device);
+            const size_t need = entry.grouped_grad_ws(dy.rows, experts);
+            if (need) ws = workspace(need, device);
+            rc = entry.grouped_grad(dy.p, dy.rows, N, dy.ld, w, (const uint8_t*)tp, K, experts, offsets, dx.data_ptr(), K, dy.dtype,
+                                    need ? ws.data_ptr() : nullptr, need, stream());
+        }
+        return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(std::move(dx));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
 // Addresses of the C entry points, in the order of Entry.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     constexpr int COUNT = sizeof(Entry) / sizeof(void*);
@@ -582,7 +828,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     entry = Entry{(w_only_fn)p[0], (w8a8_fn)p[1], (wxa8_fn)p[2], (wxa8_fn)p[3], (quantize_fn)p[4], (pack_fn)p[5], (split_bytes_fn)p[6],
                   (a8_bytes_fn)p[7], (packed_bytes_fn)p[8], (mx_bytes_fn)p[9], (mx_quantize_fn)p[10], (mx_dequantize_fn)p[11], (mx_ws_fn)p[12],
                   (mx_linear_fn)p[13], (mx_codes_fn)p[14], (mx_ws_fn)p[15], (mx_grad_fn)p[16], (norm_fn)p[17], (norm_mx_fn)p[18],
-                  (mx_bytes_fn)p[19], (norm_grad_fn)p[20]};
+                  (mx_bytes_fn)p[19], (norm_grad_fn)p[20], (heads_fn)p[21], (heads_ws_fn)p[22], (heads_grad_fn)p[23], (mx_act_fn)p[24], (mx_ws_fn)p[25],
+                  (act_grad_fn)p[26], (heads_ws_fn)p[27], (grouped_fn)p[28], (mx_bytes_fn)p[29], (grouped_grad_fn)p[30]};
     Py_RETURN_NONE;
 }
 
@@ -599,6 +846,12 @@ PyMethodDef methods[] = {
     {"mx_linear_grad", (PyCFunction)(void (*)(void))mx_linear_grad, METH_FASTCALL, nullptr},
     {"layer_norm", (PyCFunction)(void (*)(void))layer_norm, METH_FASTCALL, nullptr},
     {"layer_norm_grad", (PyCFunction)(void (*)(void))layer_norm_grad, METH_FASTCALL, nullptr},
+    {"qk_norm_rope", (PyCFunction)(void (*)(void))qk_norm_rope, METH_FASTCALL, nullptr},
+    {"qk_norm_rope_grad", (PyCFunction)(void (*)(void))qk_norm_rope_grad, METH_FASTCALL, nullptr},
+    {"mx_linear_act", (PyCFunction)(void (*)(void))mx_linear_act, METH_FASTCALL, nullptr},
+    {"act_grad", (PyCFunction)(void (*)(void))act_grad, METH_FASTCALL, nullptr},
+    {"mx_linear_grouped", (PyCFunction)(void (*)(void))mx_linear_grouped, METH_FASTCALL, nullptr},
+    {"mx_linear_grouped_grad", (PyCFunction)(void (*)(void))mx_linear_grouped_grad, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mqhost", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
