@@ -30,7 +30,9 @@ EXPORTS = ("mq_version", "mq_last_hip_error", "mq_tune_force_tile", "mq_tune_for
            "mq_bos_aware_kv_proj_workspace_bytes", "mq_bos_aware_kv_proj", "mq_alloc_solve", "mq_alloc_split_budget",
            "mq_alloc_search", "mq_mx_bytes", "mq_mx_quantize", "mq_mx_dequantize", "mq_mx_pack", "mq_mx_unpack", "mq_mx_column_top",
            "mq_mx_linear_workspace_bytes", "mq_mx_linear", "mq_mx_linear_codes", "mq_mx_linear_grad_workspace_bytes", "mq_mx_linear_grad", "mq_layer_norm", "mq_layer_norm_mx",
-           "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad")
+           "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad",
+           "mq_rotary_table", "mq_qk_norm_rope", "mq_qk_norm_rope_grad_workspace_bytes", "mq_qk_norm_rope_grad", "mq_mx_linear_act", "mq_mx_linear_act_codes", "mq_act_grad_workspace_bytes",
+           "mq_act_grad", "mq_mx_experts_column_top", "mq_mx_linear_grouped_workspace_bytes", "mq_mx_linear_grouped", "mq_mx_linear_grouped_grad_workspace_bytes", "mq_mx_linear_grouped_grad")
 
 
 class MixdqError(RuntimeError):
@@ -1047,6 +1049,8 @@ def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Te
 
 def _on_current(device) -> None:
     """Kernels are launched on the current device's stream."""
+    if device.type != "cuda":
+        raise ValueError(f"expected operands on the GPU, got them on {device}")
     if device.index != torch.cuda.current_device():
         raise ValueError(f"operands are on {device}, the current device is cuda:{torch.cuda.current_device()}")
 
@@ -1155,6 +1159,8 @@ def qk_norm_rope_grad(dy: torch.Tensor, x: Optional[torch.Tensor], q_heads: int,
     _on_current(dy.device)
     dt = _dtype_code(dy)
     if norm:
+        if x is None:
+            raise ValueError("the gradient of the norm takes its input")
         _matrix(x, *dy.shape, dy.dtype, dy.device)
     else:
         x = None

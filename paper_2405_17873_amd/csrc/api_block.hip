@@ -42,12 +42,11 @@ static bool gate_fits(int N, int K) { return (long)N * K <= 1L << 32; }
 static int check_product_act(int M, int N, int K, const void* w, const void* bias, int act, int gated, const void* y, long ldy, int dtype, const void* residual,
                              long ldr, const void* pre, long ldpre) {
     int rc;
-    if (N <= 0 || N > (1 << 22) || (gated && N % 64 != 0)) return MQ_ERR_BAD_SHAPE;
+    if (N <= 0 || N > (1 << 22) || (gated && (N % 64 != 0 || !gate_fits(N, K)))) return MQ_ERR_BAD_SHAPE;
     const int outs = gated ? N / 2 : N;
     if ((rc = check_product(M, outs, K, w, bias, y, ldy, dtype, residual, ldr)) || (rc = check_mx(w, N, K)) ||
         (rc = check_act(M, N, act, gated, y, ldy, residual, pre, ldpre)))
         return rc;
-    if (gated && !gate_fits(N, K)) return MQ_ERR_BAD_SHAPE;
     if (M > 0 && !itself_or_apart(y, ldy, residual, ldr, outs, M)) return MQ_ERR_BAD_ARG;
     if (M > 0 && pre && residual && !apart(pre, ldpre, N, residual, ldr, N, M)) return MQ_ERR_BAD_ARG;
     return MQ_OK;
@@ -81,10 +80,11 @@ int mq_rotary_table(const double* freq_host, const int* axis_host, int pairs, ui
     const long double two_pi = 6.283185307179586476925286766559005768L;
     for (int i = 0; i < pairs; ++i) {
         if (!isfinite(freq_host[i]) || axis_host[i] < 0 || axis_host[i] > 3) return MQ_ERR_BAD_ARG;
-        long double turn = (long double)freq_host[i] / two_pi;
+        long double turn = fabsl((long double)freq_host[i]) / two_pi;
         turn -= floorl(turn);
         const long double units = roundl(ldexpl(turn, 64));
-        const uint64_t f = units >= 18446744073709551616.0L ? 0 : (uint64_t)units;
+        uint64_t f = units >= 18446744073709551616.0L ? 0 : (uint64_t)units;
+        if (freq_host[i] < 0) f = 0 - f;
         table_host[4 * i] = (uint32_t)f;
         table_host[4 * i + 1] = (uint32_t)(f >> 32);
         table_host[4 * i + 2] = (uint32_t)axis_host[i];
@@ -203,11 +203,10 @@ int mq_mx_linear_grouped(const void* x, int M, int K, long ldx, const void* w, i
     if (M < 0) return MQ_ERR_BAD_SHAPE;
     int rc;
     if ((rc = check_experts(w, N, K, experts, offsets, M)) || (rc = check_matrix(x, M, ldx, K))) return rc;
-    if (gated && N % 64 != 0) return MQ_ERR_BAD_SHAPE;
+    if (gated && (N % 64 != 0 || !gate_fits(N, K))) return MQ_ERR_BAD_SHAPE;
     const int outs = gated ? N / 2 : N;
     if ((rc = check_matrix(y, M, ldy, outs)) || (rc = check_act(M, N, act, gated, y, ldy, nullptr, pre, ldpre))) return rc;
     if (!aligned(bias, 2)) return MQ_ERR_BAD_ARG;
-    if (gated && !gate_fits(N, K)) return MQ_ERR_BAD_SHAPE;
     if (M == 0) return MQ_OK;
     if (!apart(x, ldx, K, y, ldy, outs, M) || (pre && !apart(x, ldx, K, pre, ldpre, N, M))) return MQ_ERR_BAD_ARG;
     const size_t need = mq_mx_linear_grouped_workspace_bytes(M, N, K, experts);

@@ -9,10 +9,11 @@
 
 namespace mq {
 
-struct GateTerms {
-    float c, d;  // a sigma(c a + d a^3)
-};
-__device__ __forceinline__ GateTerms gate_terms(int act) { return act == MQ_ACT_SILU ? GateTerms{1.0f, 0.0f} : GateTerms{1.5957691216f, 0.0713548163f}; }
+// sigma(z) of z times -log2(e)
+__device__ __forceinline__ float gate_sigma(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z)); }
+__device__ __forceinline__ float square(float a) { return fminf(a * a, 1e30f); }  // (finite: products with zero stay zero)
+__device__ __forceinline__ float silu_sigma(float a) { return gate_sigma(a * -1.4426950409f); }
+__device__ __forceinline__ float tanh_sigma(float a) { return gate_sigma(a * __builtin_fmaf(-0.1029432397f, square(a), -2.3022081985f)); }
 
 // Phi(-|a|) and exp(-a^2 / 2)
 __device__ __forceinline__ float gelu_tail(float a, float& gauss) {
@@ -28,9 +29,6 @@ __device__ __forceinline__ float gelu_tail(float a, float& gauss) {
     p = __builtin_fmaf(p, t, 0.093178898f);
     return p * t * gauss;
 }
-__device__ __forceinline__ float gate_sigma(float a, GateTerms g) {
-    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950409f * (a * __builtin_fmaf(g.d, a * a, g.c))));
-}
 __device__ __forceinline__ float act_gelu(float a) {
     float gauss;
     const float e = gelu_tail(a, gauss);
@@ -44,9 +42,13 @@ __device__ __forceinline__ float act_and_slope(float a, int act, float& slope) {
         slope = __builtin_fmaf(a * 0.3989422804f, gauss, phi);
         return a * phi;
     }
-    const GateTerms g = gate_terms(act);
-    const float s = gate_sigma(a, g), f = a * s;
-    slope = __builtin_fmaf(f * (1.0f - s), __builtin_fmaf(3.0f * g.d, a * a, g.c), s);
+    if (act == MQ_ACT_SILU) {
+        const float s = silu_sigma(a), f = a * s;
+        slope = __builtin_fmaf(f, 1.0f - s, s);
+        return f;
+    }
+    const float s = tanh_sigma(a), f = a * s;
+    slope = __builtin_fmaf(f * (1.0f - s), __builtin_fmaf(0.2140644488f, square(a), 1.5957691216f), s);
     return f;
 }
 // n values; act is the same for the whole wave.
@@ -56,10 +58,12 @@ __device__ __forceinline__ void act_values(float* a, int act) {
     if (act == MQ_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) a[i] = act_gelu(a[i]);
-    } else {
-        const GateTerms g = gate_terms(act);
+    } else if (act == MQ_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) a[i] *= gate_sigma(a[i], g);
+        for (int i = 0; i < N; ++i) a[i] *= silu_sigma(a[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) a[i] *= tanh_sigma(a[i]);
     }
 }
 
