@@ -522,11 +522,10 @@ size_t mq_mx_linear_grouped_workspace_bytes(int M, int N, int K, int experts); /
 int mq_mx_linear_grouped(const void* x, int M, int K, long ldx, const void* w, int N, int experts, const int* offsets, const void* bias, int act, int gated,
                          void* y, long ldy, int dtype, void* pre, long ldpre, void* ws, size_t ws_bytes, void* stream);
 
-/* dX = dY W_e for the rows of each expert, as mq_mx_linear_grad; top [experts, K / 32] from mq_mx_experts_column_top. */
+/* dX = dY W_e for the rows of each expert, as mq_mx_linear_grad (without a workspace); top [experts, K / 32] from mq_mx_experts_column_top. */
 int mq_mx_experts_column_top(const void* mx, int experts, int N, int K, uint8_t* top, void* stream);
-size_t mq_mx_linear_grouped_grad_workspace_bytes(int M, int experts);
 int mq_mx_linear_grouped_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, int experts, const int* offsets, void* dx,
-                              long lddx, int dtype, void* ws, size_t ws_bytes, void* stream);
+                              long lddx, int dtype, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Bit-width allocation (host only: every pointer in this section is a HOST pointer, no GPU is touched, nothing is

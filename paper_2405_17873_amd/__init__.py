@@ -11,5 +11,5 @@ from .binding import (  # noqa: F401
     F32, MxTensor, layer_norm, layer_norm_grad, layer_norm_grad_workspace_bytes, layer_norm_mx, mx_bytes, mx_dequantize, mx_linear, mx_linear_grad, mx_linear_grad_workspace_bytes,
     mx_linear_workspace_bytes, mx_pack, mx_quantize, mx_quantize_weights, mx_unpack)
 from .binding import (  # noqa: F401
-    Rotary, act_grad, act_grad_workspace_bytes, mx_experts, mx_linear_grouped, mx_linear_grouped_grad, mx_linear_grouped_grad_workspace_bytes,
+    Rotary, act_grad, act_grad_workspace_bytes, mx_experts, mx_linear_grouped, mx_linear_grouped_grad,
     mx_linear_grouped_workspace_bytes, mx_quantize_experts, qk_norm_rope, qk_norm_rope_grad, qk_norm_rope_grad_workspace_bytes, rotary)

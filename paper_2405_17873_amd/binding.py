@@ -32,7 +32,7 @@ EXPORTS = ("mq_version", "mq_last_hip_error", "mq_tune_force_tile", "mq_tune_for
            "mq_mx_linear_workspace_bytes", "mq_mx_linear", "mq_mx_linear_codes", "mq_mx_linear_grad_workspace_bytes", "mq_mx_linear_grad", "mq_layer_norm", "mq_layer_norm_mx",
            "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad",
            "mq_rotary_table", "mq_qk_norm_rope", "mq_qk_norm_rope_grad_workspace_bytes", "mq_qk_norm_rope_grad", "mq_mx_linear_act", "mq_mx_linear_act_codes", "mq_act_grad_workspace_bytes",
-           "mq_act_grad", "mq_mx_experts_column_top", "mq_mx_linear_grouped_workspace_bytes", "mq_mx_linear_grouped", "mq_mx_linear_grouped_grad_workspace_bytes", "mq_mx_linear_grouped_grad")
+           "mq_act_grad", "mq_mx_experts_column_top", "mq_mx_linear_grouped_workspace_bytes", "mq_mx_linear_grouped", "mq_mx_linear_grouped_grad")
 
 
 class MixdqError(RuntimeError):
@@ -65,7 +65,7 @@ def load():
         lib = C.CDLL(_LIB_PATH)
         for name in ("mq_a8_row_bytes", "mq_split_workspace_bytes", "mq_builtin_workspace_bytes", "mq_conv3x3_a8_workspace_bytes", "mq_packed_bytes", "mq_qlinear_a8_workspace_bytes", "mq_qlinear_a8_geglu_dynamic_workspace_bytes", "mq_bos_aware_kv_proj_workspace_bytes",
                      "mq_mx_bytes", "mq_mx_linear_workspace_bytes", "mq_mx_linear_grad_workspace_bytes", "mq_layer_norm_grad_workspace_bytes", "mq_qk_norm_rope_grad_workspace_bytes", "mq_act_grad_workspace_bytes",
-                     "mq_mx_linear_grouped_workspace_bytes", "mq_mx_linear_grouped_grad_workspace_bytes"):
+                     "mq_mx_linear_grouped_workspace_bytes"):
             getattr(lib, name).restype = C.c_size_t
         lib.mq_prof_bracket_overhead_us.restype = C.c_double
         _lib = lib
@@ -91,7 +91,7 @@ def _load_native():
             "mq_mx_linear_workspace_bytes", "mq_mx_linear", "mq_mx_linear_codes", "mq_mx_linear_grad_workspace_bytes", "mq_mx_linear_grad",
             "mq_layer_norm", "mq_layer_norm_mx", "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad",
             "mq_qk_norm_rope", "mq_qk_norm_rope_grad_workspace_bytes", "mq_qk_norm_rope_grad", "mq_mx_linear_act", "mq_act_grad_workspace_bytes", "mq_act_grad",
-            "mq_mx_linear_grouped_workspace_bytes", "mq_mx_linear_grouped", "mq_mx_linear_grouped_grad_workspace_bytes", "mq_mx_linear_grouped_grad")))
+            "mq_mx_linear_grouped_workspace_bytes", "mq_mx_linear_grouped", "mq_mx_linear_grouped_grad")))
         _native = _mqhost
     return _native
 
@@ -1317,14 +1317,9 @@ def mx_linear_grouped(x: torch.Tensor, w: MxTensor, offsets: torch.Tensor, bias:
     return (y, pre) if want_pre else y
 
 
-def mx_linear_grouped_grad_workspace_bytes(M: int, experts: int) -> int:
-    return int(load().mq_mx_linear_grouped_grad_workspace_bytes(M, experts))
-
-
-def mx_linear_grouped_grad(dy: torch.Tensor, w: MxTensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
-                           ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+def mx_linear_grouped_grad(dy: torch.Tensor, w: MxTensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dX[r] = dY[r] . W_e, the gradient of mx_linear_grouped with respect to its rows (the quantisation passed straight through).  out shares nothing with dy."""
-    if out is None and ws is None and w.top is not None and w.experts > 0 and w.rows % w.experts == 0:
+    if out is None and w.top is not None and w.experts > 0 and w.rows % w.experts == 0:
         r = (_native or _load_native()).mx_linear_grouped_grad(dy, w.data, w.rows // w.experts, w.K, w.experts, w.top, offsets)
         if r is not None:
             return _done(r, "mq_mx_linear_grouped_grad")
@@ -1336,7 +1331,6 @@ def mx_linear_grouped_grad(dy: torch.Tensor, w: MxTensor, offsets: torch.Tensor,
     if w.top is None or w.top.numel() != w.experts * (w.K // 32) or w.top.dtype != torch.uint8 or not w.top.is_contiguous() or w.top.device != dy.device:
         raise ValueError("weights without the experts' `top`: make them with mx_quantize_experts or mx_experts")
     dx = _out(out, M, w.K, dy.dtype, dy.device)
-    ws = _mx_workspace(mx_linear_grouped_grad_workspace_bytes(M, w.experts), dy.device, ws)
     _check(load().mq_mx_linear_grouped_grad(_ptr(dy), M, N, _ld(dy), _mx_data(w, dy.device), _ptr(w.top), w.K, w.experts, _ptr(offsets), _ptr(dx), _ld(dx),
-                                            _dtype_code(dy), *_ws_args(ws), _stream()), "mq_mx_linear_grouped_grad")
+                                            _dtype_code(dy), _stream()), "mq_mx_linear_grouped_grad")
     return dx

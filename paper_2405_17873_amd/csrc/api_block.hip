@@ -218,19 +218,15 @@ int mq_mx_linear_grouped(const void* x, int M, int K, long ldx, const void* w, i
     return launch_mx_experts(g, gated, x, ldx, ws, (hipStream_t)stream);
 }
 
-size_t mq_mx_linear_grouped_grad_workspace_bytes(int M, int experts) { return M <= 0 || experts <= 0 ? 0 : up256(mx_experts_grad_workspace_bytes(M, experts)); }
-
 int mq_mx_linear_grouped_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, int experts, const int* offsets, void* dx,
-                              long lddx, int dtype, void* ws, size_t ws_bytes, void* stream) {
+                              long lddx, int dtype, void* stream) {
     if (!type_ok(dtype) || !top) return MQ_ERR_BAD_ARG;
     if (M < 0) return MQ_ERR_BAD_SHAPE;
     int rc;
     if ((rc = check_experts(w, N, K, experts, offsets, M)) || (rc = check_matrix(dy, M, lddy, N)) || (rc = check_matrix(dx, M, lddx, K))) return rc;
     if (M == 0) return MQ_OK;
-    if (!ws || !aligned(ws, 256)) return MQ_ERR_BAD_ARG;
-    if (ws_bytes < mq_mx_linear_grouped_grad_workspace_bytes(M, experts)) return MQ_ERR_WORKSPACE_TOO_SMALL;
     if (!apart(dx, lddx, K, dy, lddy, N, M)) return MQ_ERR_BAD_ARG;
-    return launch_mx_experts_grad(dy, M, N, lddy, w, top, K, experts, offsets, dx, lddx, dtype, ws, (hipStream_t)stream);
+    return launch_mx_experts_grad(dy, M, N, lddy, w, top, K, experts, offsets, dx, lddx, dtype, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -52,7 +52,7 @@ typedef int (*heads_grad_fn)(const void*, long, const void*, int, int, int, int,
 typedef int (*mx_act_fn)(const void*, int, int, long, const void*, int, const void*, int, int, void*, long, int, const void*, long, void*, long, void*, size_t, void*);
 typedef int (*act_grad_fn)(const void*, int, int, long, const void*, long, int, int, void*, long, int, float*, void*, size_t, void*);
 typedef int (*grouped_fn)(const void*, int, int, long, const void*, int, int, const int*, const void*, int, int, void*, long, int, void*, long, void*, size_t, void*);
-typedef int (*grouped_grad_fn)(const void*, int, int, long, const void*, const uint8_t*, int, int, const int*, void*, long, int, void*, size_t, void*);
+typedef int (*grouped_grad_fn)(const void*, int, int, long, const void*, const uint8_t*, int, int, const int*, void*, long, int, void*);
 
 struct Entry {
     w_only_fn w_only;
@@ -83,7 +83,6 @@ struct Entry {
     act_grad_fn act_grad;
     heads_ws_fn grouped_ws;
     grouped_fn grouped;
-    mx_bytes_fn grouped_grad_ws;
     grouped_grad_fn grouped_grad;
 } entry;
 
@@ -793,15 +792,12 @@ PyObject* mx_linear_grouped_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
             return general();
         const void* tp = top->data_ptr();
         const at::Device device = dy.t->device();
-        at::Tensor dx, ws;
+        at::Tensor dx;
         int rc;
         {
             Unlocked unlocked;
             dx = empty({dy.rows, K}, dy.t->scalar_type(), device);
-            const size_t need = entry.grouped_grad_ws(dy.rows, experts);
-            if (need) ws = workspace(need, device);
-            rc = entry.grouped_grad(dy.p, dy.rows, N, dy.ld, w, (const uint8_t*)tp, K, experts, offsets, dx.data_ptr(), K, dy.dtype,
-                                    need ? ws.data_ptr() : nullptr, need, stream());
+            rc = entry.grouped_grad(dy.p, dy.rows, N, dy.ld, w, (const uint8_t*)tp, K, experts, offsets, dx.data_ptr(), K, dy.dtype, stream());
         }
         return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(std::move(dx));
     } catch (const std::exception&) {
@@ -829,7 +825,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
                   (a8_bytes_fn)p[7], (packed_bytes_fn)p[8], (mx_bytes_fn)p[9], (mx_quantize_fn)p[10], (mx_dequantize_fn)p[11], (mx_ws_fn)p[12],
                   (mx_linear_fn)p[13], (mx_codes_fn)p[14], (mx_ws_fn)p[15], (mx_grad_fn)p[16], (norm_fn)p[17], (norm_mx_fn)p[18],
                   (mx_bytes_fn)p[19], (norm_grad_fn)p[20], (heads_fn)p[21], (heads_ws_fn)p[22], (heads_grad_fn)p[23], (mx_act_fn)p[24], (mx_ws_fn)p[25],
-                  (act_grad_fn)p[26], (heads_ws_fn)p[27], (grouped_fn)p[28], (mx_bytes_fn)p[29], (grouped_grad_fn)p[30]};
+                  (act_grad_fn)p[26], (heads_ws_fn)p[27], (grouped_fn)p[28], (grouped_grad_fn)p[29]};
     Py_RETURN_NONE;
 }
 

@@ -140,6 +140,37 @@ __device__ __forceinline__ void store8_16(uint16_t* p, uint4v v, int n) {
     }
 }
 
+// Quantisation to MXFP4 by a workgroup of 256 threads: rows 32 g .. 32 g + 31, columns 256 q .. 256 q + 255.
+// A lane converts eight consecutive values; four lanes share a block, and a wave covers 8 rows x 64 columns at a time, so that it reads
+// whole 128-byte pieces of eight rows and writes two of 128 bytes (8 neighbouring rows of one block column).  Four such steps, 256 columns, make the
+// scale word of a row and block column.  Bound by memory: 2 bytes read and 17/32 written per value.
+template <int DT>
+__device__ __forceinline__ void mx_quantize_groups(const uint16_t* x, int M, int K, long ldx, uint8_t* codes, uint8_t* scales, int kc, int kq, long g, int q) {
+    const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;  // (a wave takes eight of the rows)
+    if (g * 32 >= M) return;
+    const int j = sub * 8 + (lane >> 3), kb = (lane >> 2) & 1, part = lane & 3;
+    const long row = g * 32 + j;
+    const int k0 = q * 256 + (lane & 7) * 8;
+    const uint16_t* p = x + row * ldx + k0;
+    uint4v v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool in = row < M && k0 + 64 * i < K;  // K % 32 == 0: a block is whole or absent
+        v[i] = in ? load8_16(p + 64 * i, 8) : uint4v{0, 0, 0, 0};
+    }
+    uint32_t word = 0;
+    uint8_t* tile = codes + (g * kc + q * 4) * 1024 + (kb * 32 + j) * 16 + part * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t s = mx_scale_byte(quad_max(mx_top_16<DT>(v[i])));
+        uint32_t w = mx_codes_16<DT>(v[i], mx_scale_operand(s));
+        if (s == 255u) w = 0;
+        word |= s << (8 * i);
+        if (q * 4 + i < kc) *(uint32_t*)(tile + (long)i * 1024) = w;
+    }
+    if (part == 0) *(uint32_t*)(scales + (g * kq + q) * 256 + (kb * 32 + j) * 4) = word;
+}
+
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // Allows a kernel more than 64 KB of dynamic LDS on the current device.  `prepared`: the kernel's own.
@@ -196,8 +227,6 @@ __device__ __forceinline__ MxPlanTile mx_plan_tile(const MxRowPlan* p, int i) {
 // groups of 32 rows and its first row is inside one.
 inline long mx_plan_bound(long M, int experts, int tile_rows) { return M / tile_rows + 2 * (M < experts ? M : experts); }
 inline size_t mx_plan_bytes(long M, int experts, int tile_rows) { return (sizeof(MxRowPlan) + mx_plan_bound(M, experts, tile_rows) * sizeof(MxPlanTile) + 255) / 256 * 256; }
-// Tiles of tile_rows rows; whole_groups: that start with a whole group of 32.
-int launch_mx_plan(const int* offsets, int experts, int M, int tile_rows, bool whole_groups, MxRowPlan* plan, hipStream_t st);
 int launch_mx_quantize(const void* x, int M, int K, long ldx, int dtype, void* mx, hipStream_t st);
 int launch_mx_dequantize(const void* mx, int M, int K, int dtype, void* y, long ldy, hipStream_t st);
 int launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int M, int K, void* mx, hipStream_t st);
@@ -213,8 +242,7 @@ size_t mx_experts_workspace_bytes(long M, long N, long K, int experts);
 bool mx_rows_takes(int M, int N);
 bool mx_rows_quantizes(int M, int N, int K);
 int launch_mx_experts_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, int experts, const int* offsets, void* dx, long lddx,
-                           int dtype, void* ws, hipStream_t st);
-size_t mx_experts_grad_workspace_bytes(long M, int experts);
+                           int dtype, hipStream_t st);
 int launch_mx_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, void* dx, long lddx, int dtype, void* ws,
                    hipStream_t st);
 size_t mx_grad_workspace_bytes(long M, long N, long K);

@@ -5,6 +5,7 @@
 // weights are taken relative to the largest scale of their block column (top), and a value 2^-37 of its column's largest may go; the product is scaled
 // back at the end, exactly.  bfloat16 has the exponents, and weights go in as they are: relative ones of ordinary layers were larger, and sums of a dY
 // near the end of its range became infinite on the way to finite results.
+#include "expert_walk.h"
 #include "mx_common.h"
 
 namespace mq {
@@ -24,7 +25,8 @@ struct MxGrad {
     uint16_t* dx;
     long lddx;
     bool wide;  // rows of dY start on 16-byte boundaries
-    const MxRowPlan* plan;  // by expert: w and top are the first expert's
+    const int* offsets;  // by expert: w and top are the first expert's
+    int experts;
 };
 
 // What is added to the scale bytes of a block column with the largest scale `top`, and taken back at the end.  fp16: 6 units of the largest are 49152.
@@ -56,6 +58,18 @@ __device__ __forceinline__ float16v mx_grad_mfma(uint4v w, uint4v d, float16v c)
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, w), __builtin_bit_cast(half8, d), c, 0, 0, 0);
     else
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, d), c, 0, 0, 0);
+}
+
+// A tile of those that a walk has counted: it is at its last turn, which has the tile unless an earlier one does.
+__device__ __forceinline__ MxPlanTile expert_tile(ExpertWalk& walk, const MxGrad& g, int number, int tile_rows) {
+    if (number < walk.before) {
+        walk = ExpertWalk{};
+        for (;; walk.next()) {
+            walk.load(g.offsets, g.experts, g.M, tile_rows, 0);
+            if (number < walk.before + walk.turn_tiles) break;
+        }
+    }
+    return walk.tile(number, tile_rows);
 }
 
 // Eight sums of a block column, scaled back and rounded.
@@ -119,10 +133,17 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5;
     // whole tiles: neighbouring tiles of one row strip run on one XCD
-    const uint32_t undivided = EXPERTS ? mx_plan_tiles(g.plan) * work.col_tiles : work.whole;
+    // (by expert, the launch has as many workgroups as there can be tiles, and each finds its own)
+    ExpertWalk walk;
+    if constexpr (EXPERTS) {
+        for (;; walk.next()) {
+            walk.load(g.offsets, g.experts, g.M, TM * 32, 0);
+            if (walk.base + 64 >= g.experts) break;
+        }
+    }
+    const uint32_t undivided = EXPERTS ? (uint32_t)(walk.before + walk.turn_tiles) * work.col_tiles : work.whole;
     const bool whole = EXPERTS || blockIdx.x < work.whole;
     const uint32_t xcd = blockIdx.x & 7, more = undivided & 7;
-    // (by expert, the launch has as many workgroups as there can be tiles)
     if (EXPERTS && (blockIdx.x >> 3) >= (undivided >> 3) + (xcd < more ? 1u : 0u)) return;
     const uint32_t tile_v = whole ? xcd * (undivided >> 3) + (xcd < more ? xcd : more) + (blockIdx.x >> 3) : work.whole + (blockIdx.x - work.whole) / work.parts;
     const uint32_t tile = __builtin_amdgcn_readfirstlane(tile_v);  // (divisions are done in vector registers)
@@ -132,7 +153,7 @@ __global__ __launch_bounds__(NW * 64, 1) void mx_grad_kernel(const MxGrad g, con
     int rows_end = g.M;
     const uint8_t *codes = g.w.codes, *scales = g.w.scales, *top = g.top;
     if constexpr (EXPERTS) {
-        const MxPlanTile t = mx_plan_tile(g.plan, (int)tile_row);
+        const MxPlanTile t = expert_tile(walk, g, (int)tile_row, TM * 32);
         m0 = t.start;
         rows_end = t.end;
         codes += (long)t.expert * g.w.groups * g.w.kc * 1024;
@@ -345,8 +366,13 @@ __global__ __launch_bounds__(256) void mx_grad_any_kernel(const MxGrad g) {
     int rows_end = g.M;
     const uint8_t *codes = g.w.codes, *scales = g.w.scales, *top = g.top;
     if constexpr (EXPERTS) {
-        if (blockIdx.x >= mx_plan_tiles(g.plan)) return;
-        const MxPlanTile t = mx_plan_tile(g.plan, (int)blockIdx.x);
+        ExpertWalk walk;
+        for (;; walk.next()) {
+            walk.load(g.offsets, g.experts, g.M, BM, 0);
+            if ((int)blockIdx.x < walk.before + walk.turn_tiles) break;
+            if (walk.base + 64 >= g.experts) return;
+        }
+        const MxPlanTile t = walk.tile((int)blockIdx.x, BM);
         m0 = t.start;
         rows_end = t.end;
         codes += (long)t.expert * g.w.groups * g.w.kc * 1024;
@@ -524,12 +550,10 @@ int launch_mx_grad(const void* dy, int M, int N, long lddy, const void* w, const
     return dtype == MQ_F16 ? choose_mx_grad<MQ_F16>(g, (float*)ws, st) : choose_mx_grad<MQ_BF16>(g, (float*)ws, st);
 }
 
-// By expert: a plan of row tiles that start at the experts' first rows, and a workgroup for every tile that there can be.  Tiles of 32, 64 or 128 rows by the
-// average number of an expert's rows.
-size_t mx_experts_grad_workspace_bytes(long M, int experts) { return mx_plan_bytes(M, experts, 32); }
-
+// By expert: row tiles that start at the experts' first rows, and a workgroup for every tile that there can be.  Tiles of 32, 64 or 128 rows by the average number
+// of an expert's rows.
 template <int DT, int TM, int NW, int S>
-static int run_mx_experts_grad(const MxGrad& g, int experts, hipStream_t st) {
+static int run_mx_experts_grad(const MxGrad& g, hipStream_t st) {
     using P = GradPlan<TM, NW, S>;
     auto kernel = mx_grad_kernel<DT, TM, NW, S, true>;
     static PerDevice prepared;
@@ -537,24 +561,21 @@ static int run_mx_experts_grad(const MxGrad& g, int experts, hipStream_t st) {
     GradWork w = {};
     w.col_tiles = (uint32_t)((g.K / 32 + 3) / 4);
     w.parts = 1;
-    kernel<<<(unsigned)((mx_plan_bound(g.M, experts, TM * 32) * w.col_tiles + 7) / 8 * 8), NW * 64, P::BYTES, st>>>(g, w);
+    kernel<<<(unsigned)((mx_plan_bound(g.M, g.experts, TM * 32) * w.col_tiles + 7) / 8 * 8), NW * 64, P::BYTES, st>>>(g, w);
     MQ_HIP_CHECK_LAUNCH();
     return MQ_OK;
 }
 template <int DT>
-static int choose_mx_experts_grad(const MxGrad& g, int experts, const int* offsets, hipStream_t st) {
-    const bool any = !g.wide || g.lddy >= (1 << 22) || (long)g.w.groups * g.w.kc * 1024 >= (1L << 31);
-    const int rows = any ? 64 : g.M <= 32L * experts ? 32 : g.M <= 64L * experts ? 64 : 128;
-    if (const int rc = launch_mx_plan(offsets, experts, g.M, rows, false, (MxRowPlan*)g.plan, st)) return rc;
-    if (any) {
-        mx_grad_any_kernel<DT, true><<<dim3((unsigned)mx_plan_bound(g.M, experts, rows), (unsigned)g.w.kc), 256, 0, st>>>(g);
+static int choose_mx_experts_grad(const MxGrad& g, hipStream_t st) {
+    if (!g.wide || g.lddy >= (1 << 22) || (long)g.w.groups * g.w.kc * 1024 >= (1L << 31)) {
+        mx_grad_any_kernel<DT, true><<<dim3((unsigned)mx_plan_bound(g.M, g.experts, 64), (unsigned)g.w.kc), 256, 0, st>>>(g);
         MQ_HIP_CHECK_LAUNCH();
         return MQ_OK;
     }
-    return rows == 32 ? run_mx_experts_grad<DT, 1, 8, 3>(g, experts, st) : rows == 64 ? run_mx_experts_grad<DT, 2, 4, 5>(g, experts, st) : run_mx_experts_grad<DT, 4, 4, 3>(g, experts, st);
+    return g.M <= 32L * g.experts ? run_mx_experts_grad<DT, 1, 8, 3>(g, st) : g.M <= 64L * g.experts ? run_mx_experts_grad<DT, 2, 4, 5>(g, st) : run_mx_experts_grad<DT, 4, 4, 3>(g, st);
 }
 int launch_mx_experts_grad(const void* dy, int M, int N, long lddy, const void* w, const uint8_t* top, int K, int experts, const int* offsets, void* dx, long lddx,
-                           int dtype, void* ws, hipStream_t st) {
+                           int dtype, hipStream_t st) {
     MxGrad g = {};
     g.dy = (const uint16_t*)dy;
     g.lddy = M > 1 ? lddy : N;
@@ -567,8 +588,9 @@ int launch_mx_experts_grad(const void* dy, int M, int N, long lddy, const void* 
     g.dx = (uint16_t*)dx;
     g.lddx = lddx;
     g.wide = (M == 1 || g.lddy % 8 == 0) && (uintptr_t)dy % 16 == 0;
-    g.plan = (const MxRowPlan*)ws;
-    return dtype == MQ_F16 ? choose_mx_experts_grad<MQ_F16>(g, experts, offsets, st) : choose_mx_experts_grad<MQ_BF16>(g, experts, offsets, st);
+    g.offsets = offsets;
+    g.experts = experts;
+    return dtype == MQ_F16 ? choose_mx_experts_grad<MQ_F16>(g, st) : choose_mx_experts_grad<MQ_BF16>(g, st);
 }
 
 }  // namespace mq

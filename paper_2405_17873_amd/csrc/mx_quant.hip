@@ -3,37 +3,10 @@
 
 namespace mq {
 
-// A lane converts eight consecutive values; four lanes share a block, and a wave covers 8 rows x 64 columns at a time, so that it reads
-// whole 128-byte pieces of eight rows and writes two of 128 bytes (8 neighbouring rows of one block column).  Four such steps, 256 columns, make the
-// scale word of a row and block column.  Bound by memory: 2 bytes read and 17/32 written per value.
 template <int DT>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const uint16_t* x, int M, int K, long ldx, uint8_t* codes, uint8_t* scales,
                                                           int kc, int kq) {
-    const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
-    const int g = blockIdx.y + blockIdx.z * 65535;  // group of 32 rows; a wave takes eight of them
-    const int q = blockIdx.x;
-    if ((long)g * 32 >= M) return;
-    const int j = sub * 8 + (lane >> 3), kb = (lane >> 2) & 1, part = lane & 3;
-    const long row = (long)g * 32 + j;
-    const int k0 = q * 256 + (lane & 7) * 8;
-    const uint16_t* p = x + row * ldx + k0;
-    uint4v v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const bool in = row < M && k0 + 64 * i < K;  // K % 32 == 0: a block is whole or absent
-        v[i] = in ? load8_16(p + 64 * i, 8) : uint4v{0, 0, 0, 0};
-    }
-    uint32_t word = 0;
-    uint8_t* tile = codes + ((long)g * kc + q * 4) * 1024 + (kb * 32 + j) * 16 + part * 4;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t s = mx_scale_byte(quad_max(mx_top_16<DT>(v[i])));
-        uint32_t w = mx_codes_16<DT>(v[i], mx_scale_operand(s));
-        if (s == 255u) w = 0;
-        word |= s << (8 * i);
-        if (q * 4 + i < kc) *(uint32_t*)(tile + (long)i * 1024) = w;
-    }
-    if (part == 0) *(uint32_t*)(scales + ((long)g * kq + q) * 256 + (kb * 32 + j) * 4) = word;
+    mx_quantize_groups<DT>(x, M, K, ldx, codes, scales, kc, kq, blockIdx.y + blockIdx.z * 65535, blockIdx.x);
 }
 
 static dim3 rows_grid(int x, long groups) {

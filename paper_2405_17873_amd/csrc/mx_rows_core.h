@@ -16,12 +16,10 @@ struct MxRows {
     long ldx;
 };
 
-// KIND: of an MxGemm's.  Gated: half of the waves have the values' columns, the other half the gates'.  By expert: a workgroup (blockIdx.y: its expert)
-// takes the expert's rows, 32 at a time.
+// KIND: MX_ACT, MX_GATED.  Gated: half of the waves have the values' columns, the other half the gates'.
 template <int DT, bool MXIN, int RG, int U, int KIND>
 __global__ __launch_bounds__(512, 1) void mx_rows_kernel(const MxRows r) {
-    constexpr bool ACT = KIND & MX_ACT, GATED = KIND & MX_GATED, EXPERTS = KIND & MX_EXPERTS;
-    static_assert(!EXPERTS || (!MXIN && RG == 1), "rows by expert are quantised here");
+    constexpr bool ACT = KIND & MX_ACT, GATED = KIND & MX_GATED;
     const MxGemm& g = r.g;
     constexpr int NW = GATED ? 4 : 8, ROW = 32 + 4;  // waves to a column; of sums in LDS, in floats
     constexpr bool QUAD = MXIN && U == 4;  // steps of whole scale words
@@ -29,27 +27,10 @@ __global__ __launch_bounds__(512, 1) void mx_rows_kernel(const MxRows r) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wv = wave % NW;
     const int h = lane >> 5, j = lane & 31;
     const int kc = g.w.kc, kq = g.w.kq, outs = GATED ? g.N >> 1 : g.N;
-    long gw = GATED ? blockIdx.x + wave / NW * (g.w.groups >> 1) : blockIdx.x;
-    const uint16_t* bias = g.bias;
-    int first = 0, end = g.M;
-    if constexpr (EXPERTS) {
-        const int e = blockIdx.y;
-        first = g.offsets[e], end = g.offsets[e + 1];
-        first = __builtin_amdgcn_readfirstlane(first < 0 ? 0 : first);
-        end = __builtin_amdgcn_readfirstlane(end > g.M ? g.M : end);
-        if (first >= end) return;
-        if (bias) bias += (long)e * g.N;
-    }
-    const uint8_t *codes = g.w.codes, *scales = g.w.scales;
-    if constexpr (EXPERTS) {
-        codes += (long)blockIdx.y * g.w.groups * kc * 1024;
-        scales += (long)blockIdx.y * g.w.groups * kq * 256;
-    }
+    const int gw = GATED ? blockIdx.x + wave / NW * (g.w.groups >> 1) : blockIdx.x;
     const int c0 = QUAD ? kq * wv / NW * 4 : kc * wv / NW;
     const int c1 = QUAD ? (kq * (wv + 1) / NW * 4 < kc ? kq * (wv + 1) / NW * 4 : kc) : kc * (wv + 1) / NW;
-    const uint8_t *wc = codes + gw * kc * 1024 + lane * 16, *ws = scales + gw * kq * 256 + lane * 4;
-    do {
-    const int rows = EXPERTS && end - first > 32 ? 32 : end - first;
+    const uint8_t *wc = g.w.codes + (long)gw * kc * 1024 + lane * 16, *ws = g.w.scales + (long)gw * kq * 256 + lane * 4;
     float16v acc[RG];
 #pragma unroll
     for (int m = 0; m < RG; ++m)
@@ -85,8 +66,8 @@ __global__ __launch_bounds__(512, 1) void mx_rows_kernel(const MxRows r) {
 #pragma unroll
                 for (int m = 0; m < RG; ++m) {
                     const int k = (c + u) * 64 + h * 32;
-                    const bool in = m * 32 + j < rows && c + u < c1 && k < g.K;
-                    const uint16_t* p = r.x + (first + m * 32 + j) * r.ldx + k;
+                    const bool in = m * 32 + j < g.M && c + u < c1 && k < g.K;
+                    const uint16_t* p = r.x + (m * 32 + j) * r.ldx + k;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[u][m][i] = in ? load8_16(p + i * 8, 8) : uint4v{0, 0, 0, 0};
                 }
@@ -122,14 +103,14 @@ __global__ __launch_bounds__(512, 1) void mx_rows_kernel(const MxRows r) {
     // a lane holds, of one row, runs of four columns
 #pragma unroll
     for (int m = 0; m < RG; ++m) {
-        if (m * 32 + j < rows) {
+        if (m * 32 + j < g.M) {
             float* p = sums + (wave * RG * 32 + m * 32 + j) * ROW + 4 * h;
 #pragma unroll
             for (int t = 0; t < 4; ++t) *(float4v*)(p + 8 * t) = float4v{acc[m][4 * t], acc[m][4 * t + 1], acc[m][4 * t + 2], acc[m][4 * t + 3]};
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < rows * 4; i += 512) {  // runs of eight columns
+    for (int i = threadIdx.x; i < g.M * 4; i += 512) {  // runs of eight columns
         const int m = i >> 2, q = i & 3, n = blockIdx.x * 32 + q * 8, left = outs - n;
         if (left <= 0) continue;
         float f[8], gate[8];
@@ -144,8 +125,8 @@ __global__ __launch_bounds__(512, 1) void mx_rows_kernel(const MxRows r) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) f[e] += lo[e], f[4 + e] += hi[e];
             }
-            if (bias) {
-                const uint4v b = load8_16(bias + part * outs + n, left);
+            if (g.bias) {
+                const uint4v b = load8_16(g.bias + part * outs + n, left);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] += T16<DT>::up((uint16_t)(b[e >> 1] >> (16 * (e & 1))));
             }
@@ -153,7 +134,7 @@ __global__ __launch_bounds__(512, 1) void mx_rows_kernel(const MxRows r) {
         auto store = [&](uint16_t* p, const float* f) {
             store8_16(p, uint4v{T16<DT>::pack(f[0], f[1]), T16<DT>::pack(f[2], f[3]), T16<DT>::pack(f[4], f[5]), T16<DT>::pack(f[6], f[7])}, left);
         };
-        const long row = first + m;
+        const long row = m;
         total(0, f);
         if constexpr (GATED) total(1, gate);
         if constexpr (ACT) {
@@ -176,9 +157,6 @@ __global__ __launch_bounds__(512, 1) void mx_rows_kernel(const MxRows r) {
         }
         store(g.y + row * g.ldy + n, f);
     }
-    first += 32;
-    if (EXPERTS && first < end) __syncthreads();
-    } while (EXPERTS && first < end);
 }
 
 template <int DT, bool MXIN, int RG, int U, int KIND>
@@ -187,7 +165,7 @@ static int run_mx_rows(const MxRows& r, hipStream_t st) {
     auto kernel = mx_rows_kernel<DT, MXIN, RG, U, KIND>;
     static PerDevice prepared;
     if (const int rc = allow_lds(prepared, (const void*)kernel, BYTES)) return rc;
-    kernel<<<dim3((unsigned)((KIND & MX_GATED) ? r.g.w.groups / 2 : r.g.w.groups), (KIND & MX_EXPERTS) ? r.g.experts : 1), 512, BYTES, st>>>(r);
+    kernel<<<(unsigned)((KIND & MX_GATED) ? r.g.w.groups / 2 : r.g.w.groups), 512, BYTES, st>>>(r);
     MQ_HIP_CHECK_LAUNCH();
     return MQ_OK;
 }
