@@ -1,8 +1,8 @@
 """Tunes the norms and biases of feed-forward blocks whose linears are frozen in MXFP4, so that they follow their 16-bit originals.
 
 A block is  x + W2 gelu(W1 norm(x) + b1) + b2.  Its weights become 4-bit codes once; what is left to learn is a few vectors.  Forward: the layer norm
-writes MXFP4 directly, the linear reads it, the second linear quantises in the call and adds the skip connection.  Backward: gradients pass through
-the frozen codes and the norms down to the first block.  The output is also kept in 4 bits, as a skip connection of a UNet might be.
+writes MXFP4 directly, the linear reads it and has the activation in its epilogue, the second linear quantises in the call and adds the skip connection.
+Backward: gradients pass through the frozen codes, the activation and the norms down to the first block.  The output is also kept in 4 bits, as a skip connection of a UNet might be.
 
     python examples/tune_norms.py [--rows 4096] [--width 1280] [--hidden 5120] [--blocks 2] [--steps 100]
 """
@@ -27,21 +27,18 @@ class Block:
     def forward(self, x):
         b1, b2, gain, shift = self.learned
         n, mean, rstd = mq.layer_norm_mx(x, gain, shift, EPS, want_stats=True)
-        a = mq.mx_linear(n, self.w1, b1.to(x.dtype), dtype=x.dtype)
-        y = mq.mx_linear(F.gelu(a), self.w2, b2.to(x.dtype), residual=x)
+        h, a = mq.mx_linear(n, self.w1, b1.to(x.dtype), dtype=x.dtype, act="gelu", want_pre=True)
+        y = mq.mx_linear(h, self.w2, b2.to(x.dtype), residual=x)
         self.saved = x, mean, rstd, a
         return y
 
     def backward(self, dy):
         """Gradient of the input; gradients of `learned` in their order."""
         x, mean, rstd, a = self.saved
-        dh = mq.mx_linear_grad(dy, self.w2)
-        with torch.enable_grad():
-            leaf = a.detach().requires_grad_()
-            da, = torch.autograd.grad(F.gelu(leaf), leaf, dh)
+        da, db1 = mq.act_grad(mq.mx_linear_grad(dy, self.w2), a, "gelu")
         dn = mq.mx_linear_grad(da, self.w1)
         dx, dgain, dshift = mq.layer_norm_grad(dn, x, self.learned[2], mean, rstd, residual=dy)
-        return dx, [da.float().sum(0), dy.float().sum(0), dgain, dshift]
+        return dx, [db1, dy.float().sum(0), dgain, dshift]
 
 
 def original(x, w1, b1, w2, b2, gain, shift):

@@ -1,7 +1,7 @@
 // Activations of the microscaled linears, and their slopes, in fp32.
 //   gelu       a Phi(a) = max(a, 0) - m Phi(-m), m = |a|, with Phi(-m) = 2^(P(m) - m^2 log2(e) / 2), P of degree 7 fitted to the logarithm on [0, 6]: the tail
 //              is good to 4 10^-6 of itself.  m is held at 6 in P and in the product, where the result is below 6 10^-9: good to 2 % of itself down to -13.
-//              (With a reciprocal and an exponential, good to 5 10^-7: nine instructions more, 16384 x 640 x 5120 geglu 62 us where this takes 50.)
+//              (With a reciprocal and an exponential, good to 5 10^-7, it took nine instructions more: 16384 x 640 x 5120 geglu 62 us where silu takes 40; now 57 and 44.)
 //   gelu_tanh  a sigma(1.59577 a + 0.0713548 a^3), which is a / 2 (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3)))
 //   silu       a sigma(a)
 // Exponential and reciprocal are the hardware's (an ulp each; the argument of the exponential carries 2^-24 of its size).

@@ -173,6 +173,9 @@ static int choose_mx_experts(MxGemm g, const void* x, long ldx, void* ws, hipStr
     g.plan = plan;
     const bool odd = !mx_wide(g.y, g.ldy) || (g.pre && !mx_wide(g.pre, g.ldpre)) || (uintptr_t)g.bias % 16 != 0;
     constexpr long CUS = 256;
+    // us (bfloat16, gated, with the quantisation), tiles of 256 x 256 / 128 x 128: 16384 rows of 8 even experts, 2048 x 8192 158 / 193, uneven ones 171 / 207, of one 155 / 191;
+    // 4096 of 4, 2048 x 4096 40 / 34, 4001 of 16, 1280 x 2048 (fp16, no gate) 23 / 20.  Bands of 4 row tiles / of 8, each in the faster tiles: 158 / 177, 171 / 181, 155 / 155,
+    // 33.6 / 33.8, 19.9 / 20.1.
     const bool large = !odd && g.M / g.experts >= 512 && ((g.a.groups + 7L) / 8) * ((g.w.groups + 7L) / 8) >= 2 * CUS;
     const int rows = large ? 256 : 128;
     const long most = 65534;  // groups in one plane of the grid, behind the plan's row of it
@@ -182,7 +185,7 @@ static int choose_mx_experts(MxGemm g, const void* x, long ldx, void* ws, hipStr
     MQ_HIP_CHECK_LAUNCH();
     const long bound = mx_plan_bound(g.M, g.experts, rows);
     if (odd) return run_mx_form<DT, MX_ODD, KIND, 2, 2, 2, 2, 4>(g, 8, 1L << 31, bound, st);
-    return large ? run_mx_form<DT, MX_PLAIN, KIND, 2, 4, 4, 2, 4>(g, 8, CUS, bound, st) : run_mx_form<DT, MX_PLAIN, KIND, 2, 2, 2, 2, 4>(g, 8, 2 * CUS, bound, st);
+    return large ? run_mx_form<DT, MX_PLAIN, KIND, 2, 4, 4, 2, 4>(g, 4, CUS, bound, st) : run_mx_form<DT, MX_PLAIN, KIND, 2, 2, 2, 2, 4>(g, 4, 2 * CUS, bound, st);
 }
 
 int launch_mx_experts(const MxGemm& g, bool gated, const void* x, long ldx, void* ws, hipStream_t st) {
