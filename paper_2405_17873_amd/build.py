@@ -33,7 +33,7 @@ PER_FILE = {
     "heads.hip": ["-fno-slp-vectorize"],
 }
 SOURCES = ["api.hip", "quant_pack.hip", "act_quant.hip", "gemm.hip", "gemm_solo.hip", "gemm_panel.hip", "bos.hip", "prof.hip", "peaks.hip", "alloc.cpp",
-           "mx_quant.hip", "mx_gemm.hip", "mx_rows.hip", "mx_grad.hip", "mx_gemm_act.hip", "mx_rows_act.hip", "mx_experts.hip", "act_grad.hip", "norm.hip", "heads.hip", "api_mx.hip", "api_block.hip"]
+           "mx_quant.hip", "mx_gemm.hip", "mx_rows.hip", "mx_grad.hip", "mx_gemm_act.hip", "mx_rows_act.hip", "mx_few_rows.hip", "mx_experts.hip", "act_grad.hip", "norm.hip", "heads.hip", "api_mx.hip", "api_block.hip"]
 
 
 def _compile(src: str, force: bool) -> str:

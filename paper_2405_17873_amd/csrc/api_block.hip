@@ -59,7 +59,7 @@ static MxGemm product_act(int M, int K, const void* w, int N, const void* bias, 
 }
 static int run_act(MxGemm& g, int gated, const void* a, hipStream_t st) {
     g.a = mx_view(a, g.M, g.K);
-    return mx_rows_takes(g.M, g.N) ? launch_mx_rows_act(g, gated, nullptr, 0, st) : launch_mx_gemm_act(g, gated, st);
+    return mx_rows_takes(g.M, g.N) ? launch_mx_rows_act(g, gated, st) : launch_mx_gemm_act(g, gated, st);
 }
 // Weights of `experts` experts, N rows of each, one behind the other in one matrix.
 static int check_experts(const void* w, int N, int K, int experts, const int* offsets, int M) {
@@ -145,8 +145,8 @@ int mq_mx_linear_act(const void* x, int M, int K, long ldx, const void* w, int N
     if (M == 0) return MQ_OK;
     MxGemm g = product_act(M, K, w, N, bias, act, y, ldy, dtype, residual, ldr, pre, ldpre);
     // (one launch reads activations while others of its workgroups store results)
-    if (mx_rows_quantizes(M, N, K) && apart(x, ldx, K, y, ldy, gated ? N / 2 : N, M) && (!pre || apart(x, ldx, K, pre, ldpre, N, M)))
-        return launch_mx_rows_act(g, gated, x, ldx, (hipStream_t)stream);
+    if (mx_few_rows_takes(M, N, K) && apart(x, ldx, K, y, ldy, gated ? N / 2 : N, M) && (!pre || apart(x, ldx, K, pre, ldpre, N, M)))
+        return launch_mx_few_rows(g, gated, x, ldx, (hipStream_t)stream);
     if (!ws || !aligned(ws, 256)) return MQ_ERR_BAD_ARG;
     if (ws_bytes < up256(mx_bytes(M, K))) return MQ_ERR_WORKSPACE_TOO_SMALL;
     if ((rc = launch_mx_quantize(x, M, K, ldx, dtype, ws, (hipStream_t)stream))) return rc;

@@ -236,7 +236,9 @@ int launch_mx_column_top(const void* mx, int rows, int K, uint8_t* top, hipStrea
 int launch_mx_gemm(const MxGemm& g, hipStream_t st);
 int launch_mx_gemm_act(const MxGemm& g, bool gated, hipStream_t st);
 int launch_mx_rows(const MxGemm& g, const void* x, long ldx, hipStream_t st);  // x: 16-bit activations, or null: g.a
-int launch_mx_rows_act(const MxGemm& g, bool gated, const void* x, long ldx, hipStream_t st);
+int launch_mx_rows_act(const MxGemm& g, bool gated, hipStream_t st);
+int launch_mx_few_rows(const MxGemm& g, bool gated, const void* x, long ldx, hipStream_t st);
+bool mx_few_rows_takes(int M, int N, int K);
 int launch_mx_experts(const MxGemm& g, bool gated, const void* x, long ldx, void* ws, hipStream_t st);
 size_t mx_experts_workspace_bytes(long M, long N, long K, int experts);
 bool mx_rows_takes(int M, int N);
