@@ -48,7 +48,7 @@ extern "C" {
 
 #define MQ_F16 0
 #define MQ_BF16 1
-#define MQ_F32 2 /* parameters of the layer norm only */
+#define MQ_F32 2 /* parameters of norms only */
 /* Activations (act): none, a Phi(a), its tanh approximation, a / (1 + exp(-a)). */
 #define MQ_ACT_NONE 0
 #define MQ_ACT_GELU 1
@@ -483,7 +483,7 @@ int mq_rotary_table(const double* freq_host, const int* axis_host, int pairs, ui
  *   norm == 0: u = x, no weights.
  *   y: pair p < pairs of u, values (p, p + pairs) of the head or (2 p, 2 p + 1) if interleaved, turned by positions[m, axis p] times its frequency; the rest of u.
  * positions [M, axes] of signed integers of position_bytes (4 or 8), rows ldpos apart, axes 1 .. 4; pairs == 0: no rotation, table and positions unused.
- * y may be x.  fp32, rounded once.  head_dim a multiple of 8 up to 512, pairs a multiple of 4, q_heads and k_heads up to 4096 (one of them may be 0),
+ * y may be x.  fp32, rounded once (squares past its range make a head zero).  head_dim a multiple of 8 up to 512, pairs a multiple of 4, q_heads and k_heads up to 4096 (one of them may be 0),
  * M (q_heads + k_heads) below 2^31, otherwise MQ_ERR_BAD_SHAPE. */
 int mq_qk_norm_rope(const void* x, int M, int q_heads, int k_heads, int head_dim, long ldx, const void* q_weight, const void* k_weight, int param_dtype, float eps,
                     int norm, const void* table, int pairs, int interleaved, const void* positions, int position_bytes, int axes, long ldpos, void* y, long ldy,
