@@ -171,6 +171,21 @@ def test_heads_views(mq, M):
     assert torch.equal(mq.qk_norm_rope(x, 3, 2, rotary=rot, positions=at), mq.qk_norm_rope(x, 3, 2, rotary=rot, positions=at.view(-1, 1).int()))
 
 
+@pytest.mark.parametrize("kind", ("same", "f32"))
+def test_heads_one_weight(mq, kind):
+    """Weights of the queries or of the keys alone: the others' are 1."""
+    for dtype in TYPES:
+        c = Heads(mq, 33, 3, 2, 64, (32,), dtype == F16, dtype, kind)
+        x, dy = rand((33, 320), dtype, 22), rand((33, 320), dtype, 23)
+        both = c.w.copy()
+        for only in ("q_weight", "k_weight"):
+            args = dict(c.args, **{("k_weight" if only == "q_weight" else "q_weight"): None})
+            c.w = both.copy()
+            c.w[(slice(3, None) if only == "q_weight" else slice(0, 3))] = 1.0
+            c.check_forward(x, mq.qk_norm_rope(x, **args))
+            c.check_gradient(dy, x, *mq.qk_norm_rope_grad(dy, x, **args))
+
+
 def test_heads_special_rows(mq):
     """Zeros, infinities and NaN stay in their heads; sums of the gradient take them only where they belong."""
     c = Heads(mq, 20, 2, 2, 64, (32,), False, F16, "f32")
@@ -266,7 +281,7 @@ def check_activated(y, pre, a, e_a, name, gated, dtype, res=None):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("name", ACTS)
-@pytest.mark.parametrize("M,K,N", ((1, 32, 1), (1, 320, 1280), (3, 64, 33), (8, 1280, 96), (33, 288, 31), (64, 640, 72), (100, 480, 257), (130, 128, 130), (260, 544, 520),
+@pytest.mark.parametrize("M,K,N", ((1, 32, 1), (1, 320, 1280), (3, 64, 33), (2, 6976, 40), (31, 2048, 65), (8, 1280, 96), (33, 288, 31), (64, 640, 72), (100, 480, 257), (130, 128, 130), (260, 544, 520),
                                    (513, 320, 384)))
 def test_act(mq, M, K, N, name, dtype):
     x, w, b, r = rand((M, K), dtype, M + K), rand((N, K), dtype, N, 0.05), rand((N,), dtype, 9, 0.5), rand((M, N), dtype, 10)
@@ -280,7 +295,7 @@ def test_act(mq, M, K, N, name, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("name", ACTS)
-@pytest.mark.parametrize("M,K,N", ((1, 32, 64), (1, 320, 2560), (7, 96, 192), (33, 1280, 128), (64, 288, 320), (100, 480, 576), (130, 128, 64), (260, 544, 704), (513, 320, 1088)))
+@pytest.mark.parametrize("M,K,N", ((1, 32, 64), (1, 320, 2560), (3, 6944, 64), (32, 2080, 64), (7, 96, 192), (33, 1280, 128), (64, 288, 320), (100, 480, 576), (130, 128, 64), (260, 544, 704), (513, 320, 1088)))
 def test_gate(mq, M, K, N, name, dtype):
     x, w, b = rand((M, K), dtype, M + K), rand((N, K), dtype, N, 0.05), rand((N,), dtype, 9, 0.5)
     y, pre = check_act(mq, x, w, b, name, True)
@@ -437,7 +452,8 @@ def expert_case(M, E, K, N, dtype, sizes, seed=0):
 
 SPLITS = ((1, 1, 32, 32, (1,)), (1, 3, 64, 64, (0, 1, 0)), (5, 2, 96, 32, (0, 0)), (7, 4, 320, 96, (3, 0, 1, 2)), (40, 4, 160, 128, (33, 0, 7, 0)), (70, 2, 64, 64, (1, 66)),
           (300, 5, 288, 160, (31, 32, 33, 1, 200)), (260, 3, 128, 320, (130, 0, 129)), (1000, 2, 544, 192, (515, 470)), (500, 40, 64, 64, tuple((i * 7) % 25 for i in range(40))),
-          (900, 300, 32, 32, tuple(3 if i % 3 else 0 for i in range(300))), (640, 6, 352, 256, (5, 300, 64, 128, 0, 140)))
+          (900, 300, 32, 32, tuple(3 if i % 3 else 0 for i in range(300))), (300, 40, 64, 64, (200,) + (0,) * 38 + (70,)), (50, 8, 4192, 64, (33, 0, 5, 0, 1, 0, 0, 9)),
+          (1000, 100, 96, 64, tuple(i % 21 for i in range(100))), (1400, 130, 64, 32, (700,) + (0,) * 100 + (20,) * 29), (640, 6, 352, 256, (5, 300, 64, 128, 0, 140)))
 
 
 @pytest.mark.parametrize("dtype", TYPES)
