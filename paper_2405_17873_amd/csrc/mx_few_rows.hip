@@ -6,15 +6,15 @@ namespace mq {
 typedef int int8v __attribute__((ext_vector_type(8)));
 
 // A workgroup has 32 columns of Y (gated: and their gates', in the second half of the waves) and the rows of one expert (blockIdx.y; without offsets all of them),
-// 32 at a time.  Of a slab of 2048 k, all threads quantise the rows into LDS as the MFMAs want them, while each wave's weights, 256 k (gated 512), are on their way
+// 32 at a time.  Of a slab of 2048 k (with four waves 1024), all threads quantise the rows into LDS as the MFMAs want them, while each wave's weights, 256 k (gated 512), are on their way
 // to its registers; the waves' sums are joined in LDS in wave order.
 // Bound by the weights.  32 rows of 32 experts, 2048 x 2560 each (bfloat16, gated, 45 MB for the experts that have rows) 10.8 us (18.5 with the rows quantised by every
 // wave for itself, two steps of 64 k in flight).
-template <int DT, bool GATED>
-__global__ __launch_bounds__(512, 4) void mx_few_rows_kernel(const MxGemm g, const uint16_t* x, const long ldx) {
-    constexpr int PARTS = GATED ? 2 : 1, NW = 8 / PARTS, ROW = 32 + 4;  // NW: waves to a column; ROW: of sums, in floats
-    constexpr int SLAB = 32, TILES = SLAB / NW;  // in tiles of 64 k; TILES: a wave's
-    constexpr int CODES = SLAB * 1024, SCALES = SLAB / 4 * 256, SUMS = 8 * 32 * ROW * 4;
+template <int DT, bool GATED, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 4) void mx_few_rows_kernel(const MxGemm g, const uint16_t* x, const long ldx) {
+    constexpr int PARTS = GATED ? 2 : 1, NW = WAVES / PARTS, ROW = 32 + 4;  // NW: waves to a column; ROW: of sums, in floats
+    constexpr int SLAB = WAVES * 4, TILES = SLAB / NW;  // in tiles of 64 k; TILES: a wave's
+    constexpr int CODES = SLAB * 1024, SCALES = SLAB / 4 * 256, SUMS = WAVES * 32 * ROW * 4;
     __shared__ __attribute__((aligned(16))) uint8_t lds[CODES + SCALES > SUMS ? CODES + SCALES : SUMS];
     const int e = blockIdx.y;
     int first = g.offsets ? g.offsets[e] : 0, end = g.offsets ? g.offsets[e + 1] : g.M;
@@ -49,8 +49,8 @@ __global__ __launch_bounds__(512, 4) void mx_few_rows_kernel(const MxGemm g, con
             used = true;
             const int blocks = (kc - slab < SLAB ? kc - slab : SLAB) * 2;
 #pragma unroll 1
-            for (int i = threadIdx.x; i < rows * 64; i += 512) {
-                const int row = i >> 6, b = i & 63, k = slab * 64 + b * 32;
+            for (int i = threadIdx.x; i < rows * SLAB * 2; i += WAVES * 64) {
+                const int row = i / (SLAB * 2), b = i % (SLAB * 2), k = slab * 64 + b * 32;
                 if (b >= blocks) continue;
                 uint4v v[4];
                 const uint16_t* from = x + (first + row) * ldx + k;
@@ -133,16 +133,22 @@ __global__ __launch_bounds__(512, 4) void mx_few_rows_kernel(const MxGemm g, con
     }
 }
 
-template <int DT, bool GATED>
+template <int DT, bool GATED, int WAVES>
 static int run_mx_few_rows(const MxGemm& g, const void* x, long ldx, hipStream_t st) {
     const dim3 grid((unsigned)(GATED ? g.w.groups / 2 : g.w.groups), (unsigned)(g.offsets ? g.experts : 1));
-    mx_few_rows_kernel<DT, GATED><<<grid, 512, 0, st>>>(g, (const uint16_t*)x, ldx);
+    mx_few_rows_kernel<DT, GATED, WAVES><<<grid, WAVES * 64, 0, st>>>(g, (const uint16_t*)x, ldx);
     MQ_HIP_CHECK_LAUNCH();
     return MQ_OK;
 }
+// Eight waves, or four without a gate by expert, where there are workgroups enough.  us, eight / four: 32 rows of 32 experts, 2048 x 2560, 13.9 / 12.2, 128 of 64,
+// 2880 x 2880, 52 / 43; gated 13.0 / 12.8 and, of 5760, 79 / 80; one matrix, 8 x 1280 x 5120, 4.8 / 5.3, 32 x 2048 x 2560 gated 7.0 / 8.8.
+template <int DT>
+static int choose_mx_few_rows(const MxGemm& g, bool gated, const void* x, long ldx, hipStream_t st) {
+    if (gated) return run_mx_few_rows<DT, true, 8>(g, x, ldx, st);
+    return g.offsets ? run_mx_few_rows<DT, false, 4>(g, x, ldx, st) : run_mx_few_rows<DT, false, 8>(g, x, ldx, st);
+}
 int launch_mx_few_rows(const MxGemm& g, bool gated, const void* x, long ldx, hipStream_t st) {
-    if (g.dtype == MQ_F16) return gated ? run_mx_few_rows<MQ_F16, true>(g, x, ldx, st) : run_mx_few_rows<MQ_F16, false>(g, x, ldx, st);
-    return gated ? run_mx_few_rows<MQ_BF16, true>(g, x, ldx, st) : run_mx_few_rows<MQ_BF16, false>(g, x, ldx, st);
+    return g.dtype == MQ_F16 ? choose_mx_few_rows<MQ_F16>(g, gated, x, ldx, st) : choose_mx_few_rows<MQ_BF16>(g, gated, x, ldx, st);
 }
 
 // Whether one launch takes the product of a matrix: little work to quantise, or one slab.  us, one launch / quantised before it: 8 x 1280 x 10240 gated 5.5 / 7.9,
