@@ -782,7 +782,7 @@ def _no_graph(what: str, *ts) -> None:
     """Results carry no graph: what autograd would have to go through is refused rather than cut off from it."""
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in ts):
         raise RuntimeError(f"{what} is no part of autograd's graph: call it under torch.no_grad(), or in the forward of a torch.autograd.Function, and "
-                           "mx_linear_grad and layer_norm_grad for the gradients")
+                           "the calls named ..._grad for the gradients")
 
 
 def _out(t: Optional[torch.Tensor], rows: int, cols: int, dtype, device) -> torch.Tensor:
