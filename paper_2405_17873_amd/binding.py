@@ -90,7 +90,7 @@ def _load_native():
             "mq_split_workspace_bytes", "mq_qlinear_a8_workspace_bytes", "mq_packed_bytes", "mq_mx_bytes", "mq_mx_quantize", "mq_mx_dequantize",
             "mq_mx_linear_workspace_bytes", "mq_mx_linear", "mq_mx_linear_codes", "mq_mx_linear_grad_workspace_bytes", "mq_mx_linear_grad",
             "mq_layer_norm", "mq_layer_norm_mx", "mq_layer_norm_grad_workspace_bytes", "mq_layer_norm_grad",
-            "mq_qk_norm_rope", "mq_qk_norm_rope_grad_workspace_bytes", "mq_qk_norm_rope_grad", "mq_mx_linear_act", "mq_act_grad_workspace_bytes", "mq_act_grad",
+            "mq_qk_norm_rope", "mq_qk_norm_rope_grad_workspace_bytes", "mq_qk_norm_rope_grad", "mq_mx_linear_act", "mq_mx_linear_act_codes", "mq_act_grad_workspace_bytes", "mq_act_grad",
             "mq_mx_linear_grouped_workspace_bytes", "mq_mx_linear_grouped", "mq_mx_linear_grouped_grad")))
         _native = _mqhost
     return _native
@@ -1195,10 +1195,18 @@ def _mx_linear_act(x, w: MxTensor, bias, out, residual, ws, dtype, act, gated: b
     if act is None:
         raise ValueError("gated and want_pre go with an activation")
     code = _act_code(act, gated)
-    if out is None and ws is None and dtype is None and not packed:
-        r = (_native or _load_native()).mx_linear_act(x, w.data, w.rows, w.K, bias, residual, code, gated, want_pre)
-        if r is not None:
-            return _done(r, "mq_mx_linear_act")
+    if out is None and ws is None:
+        native = _native or _load_native()
+        if packed:
+            if x.K == w.K:
+                r = native.mx_linear_act_codes(x.data, x.rows, x.K, w.data, w.rows, bias, residual, code, gated, want_pre,
+                                               1 if dtype == torch.bfloat16 else 0 if dtype in _HALF else -1)
+                if r is not None:
+                    return _done(r, "mq_mx_linear_act_codes")
+        elif dtype is None:
+            r = native.mx_linear_act(x, w.data, w.rows, w.K, bias, residual, code, gated, want_pre)
+            if r is not None:
+                return _done(r, "mq_mx_linear_act")
     _no_graph("mx_linear", None if packed else x, bias, residual)
     if packed:
         M, K, device = x.rows, x.K, x.data.device

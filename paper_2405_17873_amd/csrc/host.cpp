@@ -51,6 +51,7 @@ typedef size_t (*heads_ws_fn)(int, int, int, int);
 typedef int (*heads_grad_fn)(const void*, long, const void*, int, int, int, int, long, const void*, const void*, int, float, int, const void*, int, int, const void*,
                              int, int, long, void*, long, int, float*, float*, void*, size_t, void*);
 typedef int (*mx_act_fn)(const void*, int, int, long, const void*, int, const void*, int, int, void*, long, int, const void*, long, void*, long, void*, size_t, void*);
+typedef int (*mx_act_codes_fn)(const void*, int, int, const void*, int, const void*, int, int, void*, long, int, const void*, long, void*, long, void*);
 typedef int (*act_grad_fn)(const void*, int, int, long, const void*, long, int, int, void*, long, int, float*, void*, size_t, void*);
 typedef int (*grouped_fn)(const void*, int, int, long, const void*, int, int, const int*, const void*, int, int, void*, long, int, void*, long, void*, size_t, void*);
 typedef int (*grouped_grad_fn)(const void*, int, int, long, const void*, const uint8_t*, int, int, const int*, void*, long, int, void*);
@@ -80,6 +81,7 @@ struct Entry {
     heads_ws_fn heads_grad_ws;
     heads_grad_fn heads_grad;
     mx_act_fn mx_act;
+    mx_act_codes_fn mx_act_codes;
     mx_ws_fn act_grad_ws;
     act_grad_fn act_grad;
     heads_ws_fn grouped_ws;
@@ -704,6 +706,38 @@ PyObject* mx_linear_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
 }
 
+// (data, M, K, w, N, bias, residual, act, gated, want_pre, dtype) -> y or (y, pre), code or None
+PyObject* mx_linear_act_codes(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        Matrix res;
+        int M, K, N, act, dtype;
+        void *x, *w, *bias;
+        bool gated, want;
+        if (n != 11 || !plain_calls() || !small_int(a[1], M) || !small_int(a[2], K) || !small_int(a[4], N) || !small_int(a[7], act) || !flag(a[8], gated) ||
+            !flag(a[9], want) || !small_int(a[10], dtype) || (dtype != 0 && dtype != 1) || !mx_data(a[0], M, K, x) || !mx_data(a[3], N, K, w, gpu_tensor(a[0])) ||
+            (gated && (N % 64 != 0 || a[6] != Py_None)) || !on_current(gpu_tensor(a[0])->device()) || in_graph({a[5], a[6]}))
+            return general();
+        const at::Device device = gpu_tensor(a[0])->device();
+        const at::ScalarType type = dtype ? at::kBFloat16 : at::kHalf;
+        at::ScalarType of_bias = type;
+        if (!vector(a[5], N, device, bias, &of_bias) || of_bias != type || !optional_matrix(a[6], M, N, dtype, device, res)) return general();
+        const int outs = gated ? N / 2 : N;
+        at::Tensor y, pre;
+        int rc;
+        {
+            Unlocked unlocked;
+            y = empty({M, outs}, type, device);
+            if (want) pre = empty({M, N}, type, device);
+            rc = entry.mx_act_codes(x, M, K, w, N, bias, act, gated, y.data_ptr(), outs, dtype, res.p, res.ld, want ? pre.data_ptr() : nullptr, N, stream());
+        }
+        if (rc) return PyLong_FromLong(rc);
+        return want ? pair_or_more({y, pre}) : THPVariable_Wrap(std::move(y));
+    } catch (const std::exception&) {
+        PyErr_Clear();
+        return general();
+    }
+}
+
 // (dy, pre, act, gated) -> (da, dbias), code or None
 PyObject* act_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     try {
@@ -825,8 +859,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     entry = Entry{(w_only_fn)p[0], (w8a8_fn)p[1], (wxa8_fn)p[2], (wxa8_fn)p[3], (quantize_fn)p[4], (pack_fn)p[5], (split_bytes_fn)p[6],
                   (a8_bytes_fn)p[7], (packed_bytes_fn)p[8], (mx_bytes_fn)p[9], (mx_quantize_fn)p[10], (mx_dequantize_fn)p[11], (mx_ws_fn)p[12],
                   (mx_linear_fn)p[13], (mx_codes_fn)p[14], (mx_ws_fn)p[15], (mx_grad_fn)p[16], (norm_fn)p[17], (norm_mx_fn)p[18],
-                  (mx_bytes_fn)p[19], (norm_grad_fn)p[20], (heads_fn)p[21], (heads_ws_fn)p[22], (heads_grad_fn)p[23], (mx_act_fn)p[24], (mx_ws_fn)p[25],
-                  (act_grad_fn)p[26], (heads_ws_fn)p[27], (grouped_fn)p[28], (grouped_grad_fn)p[29]};
+                  (mx_bytes_fn)p[19], (norm_grad_fn)p[20], (heads_fn)p[21], (heads_ws_fn)p[22], (heads_grad_fn)p[23], (mx_act_fn)p[24], (mx_act_codes_fn)p[25],
+                  (mx_ws_fn)p[26], (act_grad_fn)p[27], (heads_ws_fn)p[28], (grouped_fn)p[29], (grouped_grad_fn)p[30]};
     Py_RETURN_NONE;
 }
 
@@ -846,6 +880,7 @@ PyMethodDef methods[] = {
     {"qk_norm_rope", (PyCFunction)(void (*)(void))qk_norm_rope, METH_FASTCALL, nullptr},
     {"qk_norm_rope_grad", (PyCFunction)(void (*)(void))qk_norm_rope_grad, METH_FASTCALL, nullptr},
     {"mx_linear_act", (PyCFunction)(void (*)(void))mx_linear_act, METH_FASTCALL, nullptr},
+    {"mx_linear_act_codes", (PyCFunction)(void (*)(void))mx_linear_act_codes, METH_FASTCALL, nullptr},
     {"act_grad", (PyCFunction)(void (*)(void))act_grad, METH_FASTCALL, nullptr},
     {"mx_linear_grouped", (PyCFunction)(void (*)(void))mx_linear_grouped, METH_FASTCALL, nullptr},
     {"mx_linear_grouped_grad", (PyCFunction)(void (*)(void))mx_linear_grouped_grad, METH_FASTCALL, nullptr},

@@ -291,6 +291,7 @@ def test_act(mq, M, K, N, name, dtype):
     o = r.clone()
     assert mq.mx_linear(x, mq.mx_quantize_weights(w), b, residual=o, out=o, act=name) is o and torch.equal(o, z)
     check_act(mq, x, w, None, name, False, r, packed=True, want_pre=False)
+    check_act(mq, x, w, b, name, False, packed=True)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -399,6 +400,10 @@ def test_act_grad_values_everywhere(mq):
             da, _ = mq.act_grad(torch.ones_like(a), a, name)
             _, s, _, e_s = act_error(f64(a), name, 0.0)
             within(f64(da), s, e_s + half_step(np.abs(s) + e_s, dtype), name, dtype)
+            both, _ = mq.act_grad(torch.ones_like(a), torch.cat((torch.ones_like(a), a), 1), name, True)
+            f, _, e_f, _ = act_error(f64(a), name, 0.0)
+            within(f64(both[:, :64]), f, e_f + half_step(np.abs(f) + e_f, dtype), name, dtype)
+            assert torch.equal(both[:, 64:], da)
 
 
 def test_act_grad_views_and_aliases(mq):
