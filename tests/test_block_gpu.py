@@ -369,6 +369,35 @@ def test_act_special_values(mq):
             assert (g[1] == 0).all() and torch.isnan(g[3]).all()
 
 
+def test_act_empty(mq):
+    w = mq.mx_quantize_weights(rand((64, 64), F16, 1))
+    x = torch.empty(0, 64, dtype=F16, device="cuda")
+    assert mq.mx_linear(x, w, act="gelu").shape == (0, 64)
+    y, pre = mq.mx_linear(x, w, act="silu", gated=True, want_pre=True)
+    assert y.shape == (0, 32) and pre.shape == (0, 64)
+
+
+def test_act_deterministic_and_independent_of_neighbours(mq):
+    """The same bits twice and on streams at once; a row's result does not depend on the rows beside it."""
+    w, ex = mq.mx_quantize_weights(rand((128, 320), BF16, 9, 0.05)), mq.mx_quantize_experts(rand((2, 128, 320), BF16, 10, 0.05))
+    for M in (20, 60, 300):
+        x = rand((M, 320), BF16, 8)
+        off = torch.tensor([0, M // 2, M], dtype=torch.int32, device="cuda")
+        calls = (lambda x: mq.mx_linear(x, w, act="gelu"), lambda x: mq.mx_linear(x, w, act="gelu", gated=True), lambda x: mq.mx_linear_grouped(x, ex, off, act="silu", gated=True))
+        want = [c(x) for c in calls]
+        torch.cuda.synchronize()
+        streams, got = [torch.cuda.Stream() for _ in range(2)], []
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append([c(x) for c in calls])
+        torch.cuda.synchronize()
+        for r in got:
+            assert all(torch.equal(a, b) for a, b in zip(r, want))
+        x2 = x.clone()
+        x2[1:] = float("nan")
+        assert all(torch.equal(c(x2)[0], v[0]) for c, v in zip(calls, want))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("name", ACTS)
 @pytest.mark.parametrize("gated", (False, True))
