@@ -268,17 +268,17 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void mx_gemm_kernel(const MxGemm g
                 "s"(keeps), "n"((S - 2) * P::OPS), "n"((S - 2) * P::OPS + STORES), "n"((S - 2) * P::OPS + STORES + (ACT ? P::STORES : 0))
                 : "memory", "scc");
         else
-        asm volatile(
-            "s_cmp_lt_i32 %0, 1\n\t"
-            "s_cbranch_scc1 .Lloads%=\n\t"
-            "s_waitcnt vmcnt(%2) lgkmcnt(0)\n\t"
-            "s_branch .Lready%=\n"
-            ".Lloads%=:\n\t"
-            "s_waitcnt vmcnt(%1) lgkmcnt(0)\n"
-            ".Lready%=:\n\t"
-            "s_barrier" ::"s"(behind_stores),
-            "n"((S - 2) * P::OPS), "n"((S - 2) * P::OPS + STORES)
-            : "memory", "scc");
+            asm volatile(
+                "s_cmp_lt_i32 %0, 1\n\t"
+                "s_cbranch_scc1 .Lloads%=\n\t"
+                "s_waitcnt vmcnt(%2) lgkmcnt(0)\n\t"
+                "s_branch .Lready%=\n"
+                ".Lloads%=:\n\t"
+                "s_waitcnt vmcnt(%1) lgkmcnt(0)\n"
+                ".Lready%=:\n\t"
+                "s_barrier" ::"s"(behind_stores),
+                "n"((S - 2) * P::OPS), "n"((S - 2) * P::OPS + STORES)
+                : "memory", "scc");
     };
     ready(0);
     Frag f0, f1;
