@@ -237,6 +237,7 @@ __global__ __launch_bounds__(256) void heads_kernel(const HeadArgs a) {
         if (at.more(a)) fetch();
 #pragma unroll
         for (int t = 0; t < U; ++t) {
+            if (base + t * G >= h1) break;  // (nothing left: 4096 x 40 heads of 64 10.2 -> 9.0 us, 21230 x 2 of 32 21.8 -> 14.5)
             const int h = base + t * G + grp;
             HeadUnit u = lane.template widen<DT>(v[t]);
             if (a.norm) {
@@ -307,6 +308,7 @@ __global__ __launch_bounds__(HG_WAVES * 64) void heads_grad_kernel(const HeadArg
         if (at.more(a)) fetch();
 #pragma unroll
         for (int t = 0; t < U; ++t) {
+            if (base + t * G >= h1) break;
             const int h = base + t * G + grp;
             const bool is_q = h < a.q, live = h < h1;
             const HeadUnit d = lane.template widen<DT>(dv[t]);
