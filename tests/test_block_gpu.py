@@ -774,3 +774,47 @@ def test_refusals(mq):
     for call in bad:
         with pytest.raises((ValueError, TypeError, mq.MixdqError)):
             call()
+
+
+def gelu_bounds(a):
+    """gelu and its slope, and what the kernels' are off by before they are rounded.  The tail's polynomial is fitted to 6.1e-7 max(1, 0.144 a^2) of it (1.5 a^2 U
+    past 2.6); its argument, its terms and the product count 16 U at most; the exponential's argument, two products, carries 2.5 U of 0.73 a^2 log 2.  Below
+    2^-126 exponentials are zero: 0.4 of that with |a| up to 14, and so 1e-37."""
+    t, g, f, s = ob.tail(a), ob.gauss(a), ob.act(a, "gelu"), ob.slope(a, "gelu")
+    e_t = t * (6.2e-7 + (3 * a * a + 16) * U)
+    return f, s, np.abs(a) * e_t + U * np.abs(f) + 1e-37, e_t + np.abs(a) * g * (1.5 * a * a + 5) * U + U * np.abs(s) + 2e-37
+
+
+def finite_values(dtype):
+    p = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(dtype)
+    return p[torch.isfinite(p.float())]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gelu_of_every_value(mq, dtype):
+    """All finite 16-bit arguments, from a bias behind weights of zero, in the kernels for few rows, for some, for tiles and for large tiles, whole and gated: the
+    definition's value, rounded, far down the negative side too."""
+    p = finite_values(dtype).cuda()
+    with np.errstate(over="ignore", under="ignore"):
+        f, _, e, _ = gelu_bounds(f64(p))
+    bound = e + half_step(np.abs(f) + e, dtype)
+    ones = torch.ones_like(p)
+    for bias, gated in ((p, False), (torch.cat((ones, p)), True)):
+        w = mq.mx_quantize_weights(torch.zeros(len(bias), 32, dtype=dtype, device="cuda"))
+        for M in (1, 40, 200, 600):
+            y = mq.mx_linear(torch.zeros(M, 32, dtype=dtype, device="cuda"), w, bias, act="gelu", gated=gated)
+            assert torch.equal(y, y[:1].expand_as(y))
+            within(f64(y[0]), f, bound, f"{M} rows", dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gelu_grad_of_every_value(mq, dtype):
+    a = finite_values(dtype).view(-1, 64).cuda()
+    ones = torch.ones_like(a)
+    with np.errstate(over="ignore", under="ignore"):
+        f, s, e_f, e_s = gelu_bounds(f64(a))
+    da, _ = mq.act_grad(ones, a, "gelu")
+    within(f64(da), s, e_s + half_step(np.abs(s) + e_s, dtype), "slope", dtype)
+    both, _ = mq.act_grad(ones, torch.cat((ones, a), 1), "gelu", True)
+    within(f64(both[:, :64]), f, e_f + half_step(np.abs(f) + e_f, dtype), "gate", dtype)
+    assert torch.equal(both[:, 64:], da)
