@@ -490,7 +490,8 @@ int mq_qk_norm_rope(const void* x, int M, int q_heads, int k_heads, int head_dim
                     int dtype, void* stream);
 
 /* Its gradient: dx, and the sums for the weights over rows and heads (fp32 [head_dim], each nullable; in a fixed order; zero without rows).  x: the input of the
- * forward call (unused, may be null, if norm == 0: then there are no weights either).  dx may be dy or x.  The workspace is for the sums of the weights only. */
+ * forward call (unused, may be null, if norm == 0: then there are no weights either); heads that are zero because their squares pass fp32's range have the gradient
+ * zero.  dx may be dy or x.  The workspace is for the sums of the weights only. */
 size_t mq_qk_norm_rope_grad_workspace_bytes(int M, int q_heads, int k_heads, int head_dim);
 int mq_qk_norm_rope_grad(const void* dy, long lddy, const void* x, int M, int q_heads, int k_heads, int head_dim, long ldx, const void* q_weight,
                          const void* k_weight, int param_dtype, float eps, int norm, const void* table, int pairs, int interleaved, const void* positions,

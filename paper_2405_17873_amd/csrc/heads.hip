@@ -4,7 +4,7 @@
 // apart, or, past the R values that turn, eight values.  Both values of a pair are in one lane, and a lane's pairs are the same in every head of a row, so that an
 // angle's sine and cosine are computed once for the heads that a wave takes of a row.  Waves walk over the rows; what depends on the lane alone stays in registers.
 //   y = T(x r w), r = 1 / sqrt(mean x^2 + eps), T the rotation of pair p by angle position[axis p] f_p
-//   g = T^-1 dy, dw = sum g x r, dx = r (g w - x r^2 mean(g w x))
+//   g = T^-1 dy, dw = sum g x r, dx = r (g w - x r mean(g w x r))
 // Bound by memory.  us a call among others (bfloat16): forward 32768 x 40 heads of 64, three axes 63 (5.3 TB/s), 4096 x 40 of 128 14.6, gradient 98 and 25, 4 of it joining
 // the sums.  (Lanes with three or five units each, so that none is idle with heads of 96 or 80, needed 200 registers and more: 2964 x 32 heads of 80 50; sine and cosine
 // as polynomials, weights and table once per row 90 where the first takes 63.)
@@ -319,23 +319,26 @@ __global__ __launch_bounds__(HG_WAVES * 64) void heads_grad_kernel(const HeadArg
                 g.im[j] = lane.turns ? d.im[j] * c[j] - d.re[j] * s[j] : d.im[j];
             }
             if (a.norm) {
-                const HeadUnit v = lane.template widen<DT>(xv[t]);
+                HeadUnit v = lane.template widen<DT>(xv[t]);
                 float sq = 0.0f, dot = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    sq += v.re[j] * v.re[j] + v.im[j] * v.im[j];
-                    dot += g.re[j] * either(is_q, wq.re[j], wk.re[j]) * v.re[j] + g.im[j] * either(is_q, wq.im[j], wk.im[j]) * v.im[j];
-                }
-                const float r = rsqrtf(lane_sum<L>(sq) * mean + a.eps), back = lane_sum<L>(dot) * mean * r * r;
+                for (int j = 0; j < 4; ++j) sq += v.re[j] * v.re[j] + v.im[j] * v.im[j];
                 // (of lanes that hold no head only zeros come: but 0 r is none where r is infinite, as without eps)
-                const float rl = live ? r : 0.0f;
+                const float all = rsqrtf(lane_sum<L>(sq) * mean + a.eps), r = live ? all : 0.0f;
+                // (x r and r w in the products: where squares pass float32 r is 0, and so is what comes of it; products with x itself may be infinite.)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float dr = g.re[j] * v.re[j] * rl, di = g.im[j] * v.im[j] * rl;
+                    v.re[j] *= r, v.im[j] *= r;
+                    const float dr = g.re[j] * v.re[j], di = g.im[j] * v.im[j];
                     sums[0].re[j] += either(is_q, dr, 0.0f), sums[0].im[j] += either(is_q, di, 0.0f);
                     sums[1].re[j] += either(is_q, 0.0f, dr), sums[1].im[j] += either(is_q, 0.0f, di);
-                    g.re[j] = r * (g.re[j] * either(is_q, wq.re[j], wk.re[j]) - v.re[j] * back);
-                    g.im[j] = r * (g.im[j] * either(is_q, wq.im[j], wk.im[j]) - v.im[j] * back);
+                    dot += dr * either(is_q, wq.re[j], wk.re[j]) + di * either(is_q, wq.im[j], wk.im[j]);
+                }
+                const float back = lane_sum<L>(dot) * mean * r;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    g.re[j] = g.re[j] * (r * either(is_q, wq.re[j], wk.re[j])) - v.re[j] * back;
+                    g.im[j] = g.im[j] * (r * either(is_q, wq.im[j], wk.im[j])) - v.im[j] * back;
                 }
             }
             dx.store(lane, h * a.D, live && lane.in, lane.template pack<DT>(g));

@@ -818,3 +818,23 @@ def test_gelu_grad_of_every_value(mq, dtype):
     both, _ = mq.act_grad(ones, torch.cat((ones, a), 1), "gelu", True)
     within(f64(both[:, :64]), f, e_f + half_step(np.abs(f) + e_f, dtype), "gate", dtype)
     assert torch.equal(both[:, 64:], da)
+
+
+@pytest.mark.parametrize("interleaved", (False, True))
+def test_heads_squares_past_float32(mq, interleaved):
+    """Finite heads whose squares pass float32 become zeros, forward and backward, add nothing to the weights' sums, and leave the others alone."""
+    c = Heads(mq, 24, 2, 2, 64, (16,), interleaved, BF16, "f32")
+    x, dy = rand((24, 256), BF16, 24), rand((24, 256), BF16, 25)
+    calm, calm_dy = x.clone(), dy.clone()
+    big = {(1, 0): 2.0 ** 66, (2, 1): 2.0 ** 100, (5, 3): 2.0 ** 127, (6, 2): -(2.0 ** 126)}
+    for (m, h), v in big.items():
+        x[m, 64 * h:64 * h + 64] = v
+        calm[m, 64 * h:64 * h + 64] = 0.0
+        calm_dy[m, 64 * h:64 * h + 64] = 0.0
+    y, z = mq.qk_norm_rope(x, **c.args), mq.qk_norm_rope(calm, **c.args)
+    assert torch.equal(y, z)
+    (dx, dq, dk), (cx, cq, ck) = mq.qk_norm_rope_grad(dy, x, **c.args), mq.qk_norm_rope_grad(calm_dy, calm, **c.args)
+    for m, h in big:
+        assert not dx[m, 64 * h:64 * h + 64].any()
+    assert torch.equal(dx, cx) and torch.equal(dq, cq) and torch.equal(dk, ck)
+    c.check_gradient(calm_dy, calm, dx, dq, dk)
