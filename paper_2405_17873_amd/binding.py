@@ -1270,6 +1270,7 @@ def mx_experts(t: MxTensor, experts: int) -> MxTensor:
     """A microscaled matrix as the weights of `experts` experts, one's rows behind another's, a multiple of 32 rows each; with what the gradient needs."""
     if experts <= 0 or t.rows % (32 * experts):
         raise ValueError(f"{t.rows} rows are no {experts} experts of a multiple of 32 rows")
+    _on_current(t.data.device)
     data = _mx_data(t)
     top = torch.empty((experts, t.K // 32), dtype=torch.uint8, device=t.data.device)
     _check(load().mq_mx_experts_column_top(data, experts, t.rows // experts, t.K, _ptr(top), _stream()), "mq_mx_experts_column_top")
@@ -1280,6 +1281,7 @@ def mx_quantize_experts(w: torch.Tensor) -> MxTensor:
     """Weights [experts, N, K] fp16/bf16, N % 32 == 0, for mx_linear_grouped and its gradient."""
     if w.dim() != 3:
         raise ValueError(f"expected weights [experts, N, K], got {tuple(w.shape)}")
+    _on_current(w.device)
     return mx_experts(mx_quantize(w.reshape(w.shape[0] * w.shape[1], w.shape[2])), w.shape[0])
 
 

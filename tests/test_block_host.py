@@ -241,3 +241,18 @@ def test_python_refusals(lib):
     for bad in ("relu", "GELU", 1):
         with pytest.raises(ValueError):
             mq.mx_linear(x, w, act=bad)
+
+
+def test_experts_on_another_device(lib, monkeypatch):
+    """Weights on another device than the current one are refused before anything is allocated or launched there."""
+    import torch
+    from types import SimpleNamespace as Object
+
+    import paper_2405_17873_amd as mq
+    device = torch.device("cuda:1")
+    buffer = Object(device=device, dtype=torch.uint8, is_cuda=True, is_contiguous=lambda: True, numel=lambda: 1 << 20, stride=lambda: (1,), data_ptr=lambda: 0)
+    weights = Object(device=device, shape=(2, 32, 32), dim=lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for call in (lambda: mq.mx_experts(mq.MxTensor(buffer, 64, 64), 2), lambda: mq.mx_quantize_experts(weights)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
