@@ -764,7 +764,14 @@ class MxTensor:
         return (self.rows, self.K)
 
 
+def _sizes(*n: int) -> None:
+    """The entry points take 32-bit sizes; larger ones would reach them cut off."""
+    if max(n) > 0x7FFFFFFF:
+        raise ValueError(f"sizes are below 2^31, got {n}")
+
+
 def _matrix(t: torch.Tensor, rows=None, cols=None, dtype=None, device=None) -> torch.Tensor:
+    _sizes(*t.shape, 0)
     if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
         raise ValueError(f"rows overlap: {tuple(t.shape)} with strides {t.stride()}; contiguous() makes a matrix of it")
     if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
@@ -806,6 +813,7 @@ def _vector(t: Optional[torch.Tensor], n: int, dtype, device) -> Optional[torch.
 
 def _mx_data(t: MxTensor, device=None):
     """Address of a microscaled matrix, which may have been made or moved by hand."""
+    _sizes(t.rows, t.K)
     d, need = t.data, mx_bytes(t.rows, t.K)
     if d.dtype != torch.uint8 or not d.is_contiguous() or d.numel() < need:
         raise ValueError(f"a microscaled matrix of {t.rows} x {t.K} has {need} contiguous bytes, got {d.numel()} of {d.dtype} with strides {d.stride()}")
@@ -829,6 +837,7 @@ def mx_bytes(rows: int, K: int) -> int:
 
 
 def _new_mx(rows: int, K: int, device) -> MxTensor:
+    _sizes(rows, K)
     n = mx_bytes(rows, K)
     if K <= 0 or K % 32:
         raise ValueError(f"microscaled matrices have a multiple of 32 columns, got {K}")
@@ -865,8 +874,9 @@ def mx_dequantize(t: MxTensor, dtype=torch.bfloat16, out: Optional[torch.Tensor]
         r = (_native or _load_native()).mx_dequantize(t.data, t.rows, t.K, 0 if dtype == torch.float16 else 1 if dtype == torch.bfloat16 else -1)
         if r is not None:
             return _done(r, "mq_mx_dequantize")
+    data = _mx_data(t)
     y = _out(out, t.rows, t.K, dtype, t.data.device)
-    _check(load().mq_mx_dequantize(_mx_data(t), t.rows, t.K, _dtype_code(y), _ptr(y), _ld(y), _stream()), "mq_mx_dequantize")
+    _check(load().mq_mx_dequantize(data, t.rows, t.K, _dtype_code(y), _ptr(y), _ld(y), _stream()), "mq_mx_dequantize")
     return y
 
 

@@ -256,3 +256,20 @@ def test_experts_on_another_device(lib, monkeypatch):
     for call in (lambda: mq.mx_experts(mq.MxTensor(buffer, 64, 64), 2), lambda: mq.mx_quantize_experts(weights)):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+def test_sizes_past_32_bits(lib):
+    """2^32 + 4 rows are refused, not taken for 4: matrices without memory behind them, and a microscaled one made by hand."""
+    import torch
+
+    import paper_2405_17873_amd as mq
+    rows = 2 ** 32 + 4
+    t = torch.empty(rows, 64, dtype=torch.float16, device="meta")
+    w = mq.MxTensor(torch.zeros(mq.mx_bytes(64, 64), dtype=torch.uint8), 64, 64, torch.zeros(2, dtype=torch.uint8))
+    off = torch.zeros(2, dtype=torch.int32)
+    for call in (lambda: mq.qk_norm_rope(t, 1, 1), lambda: mq.qk_norm_rope_grad(t, t, 1, 1), lambda: mq.mx_linear(t, w, act="gelu"), lambda: mq.act_grad(t, t, "silu"),
+                 lambda: mq.mx_linear_grouped(t, w, off), lambda: mq.mx_linear_grouped_grad(t, w, off), lambda: mq.mx_linear(t, w), lambda: mq.mx_linear_grad(t, w),
+                 lambda: mq.layer_norm(t), lambda: mq.mx_quantize(t), lambda: mq.mx_dequantize(mq.MxTensor(w.data, rows, 64)),
+                 lambda: mq.mx_pack(torch.empty(rows, 32, dtype=torch.uint8, device="meta"), torch.empty(rows, 2, dtype=torch.uint8, device="meta"))):
+        with pytest.raises(ValueError, match="below 2.31"):
+            call()
