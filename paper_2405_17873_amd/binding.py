@@ -874,9 +874,9 @@ def mx_dequantize(t: MxTensor, dtype=torch.bfloat16, out: Optional[torch.Tensor]
         r = (_native or _load_native()).mx_dequantize(t.data, t.rows, t.K, 0 if dtype == torch.float16 else 1 if dtype == torch.bfloat16 else -1)
         if r is not None:
             return _done(r, "mq_mx_dequantize")
-    data = _mx_data(t)
+    _sizes(t.rows, t.K)
     y = _out(out, t.rows, t.K, dtype, t.data.device)
-    _check(load().mq_mx_dequantize(data, t.rows, t.K, _dtype_code(y), _ptr(y), _ld(y), _stream()), "mq_mx_dequantize")
+    _check(load().mq_mx_dequantize(_mx_data(t), t.rows, t.K, _dtype_code(y), _ptr(y), _ld(y), _stream()), "mq_mx_dequantize")
     return y
 
 
