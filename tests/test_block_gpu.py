@@ -838,3 +838,41 @@ def test_heads_squares_past_float32(mq, interleaved):
         assert not dx[m, 64 * h:64 * h + 64].any()
     assert torch.equal(dx, cx) and torch.equal(dq, cq) and torch.equal(dk, ck)
     c.check_gradient(calm_dy, calm, dx, dq, dk)
+
+
+@pytest.mark.parametrize("interleaved", (False, True))
+@pytest.mark.parametrize("near", (2 ** 32, -(2 ** 32), 2 ** 44, -(2 ** 44), 2 ** 62, -(2 ** 62)))
+def test_heads_positions_of_two_words(mq, near, interleaved):
+    """Positions past 32 bits: the oracle's angle is the table's fraction of a turn times the position, modulo a turn, in whole numbers."""
+    M = 30
+    c = Heads(mq, M, 2, 1, 64, (12, 16), interleaved, F16, pos_type=torch.int64)
+    g = torch.Generator().manual_seed(abs(near) % 1000003)
+    c.pos.copy_(near + torch.randint(-10 ** 6, 10 ** 6, (M, 2), generator=g))
+    table, pos = c.rot.table.cpu().numpy().view(np.uint32), c.pos.tolist()
+    turn = [[((int(lo) | int(hi) << 32) * pos[m][int(axis)]) % 2 ** 64 for lo, hi, axis, _ in table] for m in range(M)]
+    c.angle = np.array(turn, np.float64) * (2 * np.pi / 2 ** 64)
+    c.far_angle = lambda: 2.0 ** -50  # (of the oracle's conversion and product)
+    x, dy = rand((M, 192), F16, 26), rand((M, 192), F16, 27)
+    c.check_forward(x, mq.qk_norm_rope(x, **c.args))
+    c.check_gradient(dy, x, *mq.qk_norm_rope_grad(dy, x, **c.args))
+
+
+def test_experts_weights_past_32_bits_are_the_first_ones(mq):
+    """The same weights as the first expert's and as those of the last, past 2^32 bytes: the same bits, of small blocks too."""
+    E, N, K = 34, 8192, 32768
+    one = mq.mx_quantize_weights(rand((N, K), F16, 1, 0.02) * torch.logspace(-2, 0, K // 32, 2.0, device="cuda").repeat_interleave(32).half())
+    codes = N // 32 * (K // 64) * 1024
+    scales = one.data.numel() - codes
+    results = []
+    for e in (0, E - 1):
+        data = torch.zeros(mq.mx_bytes(E * N, K), dtype=torch.uint8, device="cuda")
+        data[e * codes:(e + 1) * codes] = one.data[:codes]
+        data[E * codes + e * scales:E * codes + (e + 1) * scales] = one.data[codes:]
+        w = mq.mx_experts(mq.MxTensor(data, E * N, K), E)
+        for M in (3, 300):
+            x, dy = rand((M, K), F16, 2), rand((M, N), F16, 3)
+            off = torch.tensor([0] * (e + 1) + [M] * (E - e), dtype=torch.int32, device="cuda")
+            results += [mq.mx_linear_grouped(x, w, off), mq.mx_linear_grouped_grad(dy, w, off)]
+        del w, data
+    for a, b in zip(results[:4], results[4:]):
+        assert a.any() and torch.equal(a, b)
