@@ -1,8 +1,9 @@
 // Gradient of a linear's activation or gate, and of its bias.
 //   y = act(a): da = dy act'(a);  y = v act(g): dv = dy act(g), dg = dy v act'(g);  dbias = sums of da's float32 values over the rows.
 // A thread has eight columns of Y and walks down a strip of rows; a workgroup of 32 x 8 threads joins its eight rows' sums in LDS in order, and a second kernel
-// those of the strips.  Bound by memory: 2 bytes of dy, of the sums and of da per value.  4096 x 10240 gated, bfloat16: 38.5 us with the second kernel (5.4 TB/s; 58 with
-// loads in branches and none ahead), 2964 x 1280 8.7.  Workgroups in all 512 / 1024 / 2048 / 4096: 40.8 / 39.5 / 38.5 / 41.5.
+// those of the strips.  Bound by memory: 2 bytes of dy, of the sums and of da per value.  4096 x 10240 gated, bfloat16, among others: 41 us (5.1 TB/s), 46 with
+// the second kernel; 2964 x 1280 5.2 and 9.0.  Earlier, on another card, 38.5 with the second kernel, 58 with loads in branches and none ahead, and with 512 / 1024 / 2048 / 4096
+// workgroups in all 40.8 / 39.5 / 38.5 / 41.5.
 #include "mx_act.h"
 
 namespace mq {

@@ -5,9 +5,9 @@
 // angle's sine and cosine are computed once for the heads that a wave takes of a row.  Waves walk over the rows; what depends on the lane alone stays in registers.
 //   y = T(x r w), r = 1 / sqrt(mean x^2 + eps), T the rotation of pair p by angle position[axis p] f_p
 //   g = T^-1 dy, dw = sum g x r, dx = r (g w - x r mean(g w x r))
-// Bound by memory.  us a call among others (bfloat16): forward 32768 x 40 heads of 64, three axes 63 (5.3 TB/s), 4096 x 40 of 128 14.6, gradient 98 and 25, 4 of it joining
-// the sums.  (Lanes with three or five units each, so that none is idle with heads of 96 or 80, needed 200 registers and more: 2964 x 32 heads of 80 50; sine and cosine
-// as polynomials, weights and table once per row 90 where the first takes 63.)
+// Bound by memory.  us a call among others (bfloat16): forward 32768 x 40 heads of 64, three axes 62 (5.4 TB/s), 4096 x 40 of 128 14.6, gradient 103 and 27 to 30, 4 of it joining
+// the sums; 64-bit positions the same; the rotation alone 60 and 13.8.  (Lanes with three or five units each, so that none is idle with heads of 96 or 80, needed 200
+// registers and more: 2964 x 32 heads of 80 50; sine and cosine as polynomials, weights and table once per row 90 where the first takes 63.)
 // Angles: f / (2 pi) is a 64-bit fraction of a turn; its product with a position, modulo one turn, is exact integer arithmetic however far the position is.
 #include "lane_sum.h"
 #include "mx_common.h"
@@ -379,12 +379,15 @@ __global__ __launch_bounds__(256) void heads_join_kernel(const float* partial, i
     }
 }
 
-// Workgroups of the gradient, and so parts of its sums: at most as many as the chip holds at once.
+// Workgroups of the gradient, and so parts of its sums: two for each compute unit at most, which hold them at once with up to 128 registers.  (With four lanes, not interleaved,
+// it has 147: one at a time, two rounds; 21230 x 2 heads of 32 27 us, where idle lanes count too.)
 static long heads_grad_workgroups(long tasks) {
     const long n = (tasks + HG_WAVES - 1) / HG_WAVES;
     return n < 512 ? n : 512;
 }
-// Waves for every row: as many as bring the launch to 4096 (16 per compute unit), but no part of a turn's heads.  us, 2048 / 4096 / 8192 waves: forward 2964 x 32 heads
+// Waves for every row: as many as bring the launch to 4096 (16 per compute unit) or, with 2049 to 4095 rows, past it, where some take two tasks; but no part of a turn's heads.
+// Just past 4096 rows some take a second whole one: forward and gradient of 40 heads of 64, 2964 rows 7.4, 14.1, 4096 8.3, 16.3, 4200 8.8, 18.9, 6000 11.1, 20.3; of 128 11.4, 20.4,
+// 14.2, 26.9, 15.6, 30.3, 23.0, 37.9.  us, 2048 / 4096 / 8192 waves: forward 2964 x 32 heads
 // of 80 8.4 / 8.7 / 11.0, 4096 x 40 of 128 14.5 / 14.6 / 15.8, 32768 x 40 of 64 65 / 63 / 63; gradient 19.9 / 16.7 / 21.6, 24.8 / 24.9 / 26.0, 96 / 98 / 98.
 static void heads_chunks(HeadArgs& a, int L) {
     const int H = a.q + a.k, G = 64 / L, turns = (H + G - 1) / G;

@@ -1,8 +1,8 @@
 // Activations of the microscaled linears, and their slopes, in fp32.
 //   gelu       a Phi(a) = max(a, 0) - m Phi(-m), m = |a|, with Phi(-m) = exp(-m^2 / 2) P(t), t = 1 / (1 + 0.29 m), P of degree 6 fitted on [0, 13] to 6.1 10^-7 of
-//              the tail up to 2.6 and 8.7 10^-8 m^2 of it behind, half of what the exponential's argument carries there.  So negative results keep their relative
-//              accuracy down to the smallest float32.  (As one exponential of a polynomial on [0, 6], held behind it, bfloat16 results were off by 0.7 %
-//              at -7 and 2 % at -13; 16384 x 640 x 5120 geglu took 51 to 57 us, by box, where it takes 55 to 63.)
+//              the tail up to 2.6 and 8.7 10^-8 m^2 of it behind, about what the exponential's argument carries there.  So negative results keep their relative
+//              accuracy down to the smallest normal float32.  (As one exponential of a polynomial on [0, 6], held behind it, bfloat16 results were off by 0.7 %
+//              at -7 and 2 % at -13; 16384 x 640 x 5120 geglu took 51 to 57 us, by card, where it takes 55 to 63.)
 //   gelu_tanh  a sigma(1.59577 a + 0.0713548 a^3), which is a / 2 (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3)))
 //   silu       a sigma(a)
 // Exponential and reciprocal are the hardware's (an ulp each; the argument of the exponential carries 2^-24 of its size).

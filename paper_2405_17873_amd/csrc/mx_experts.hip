@@ -29,7 +29,9 @@ __global__ __launch_bounds__(256) void mx_quantize_plan_kernel(const uint16_t* x
 
 // Few rows of an expert: see mx_few_rows_kernel.  us (bfloat16), that / tiles, for 4, 8, 16 and 32 rows to an expert (uneven): 32 experts of 2048 x 2560, gated 17 / 19, 21 / 22,
 // 28 / 23, 42 / 24; 8 of 2048 x 4096, gated 11.0 / 13.0 (8 rows), 13.2 / 13.9, 18.9 / 14.1; 64 of 1280 x 1280 15.0 / 17.1, 17.7 / 17.2, 25.7 / 17.7.  (Few experts with a long
-// reduction would turn earlier: 64 rows of 4, 6400 x 1408, 23.0 / 21.5.)
+// reduction would turn earlier: 64 rows of 4, 6400 x 1408, 23.0 / 21.5.)  The host does not know how uneven the rows are.  With all of them one expert's it passes over them 32 at a time,
+// reading the weights again: 256 rows of 32 experts, 2048 x 2560, gated 37 (even 21; one row more, and so in tiles, 12 and 23), 512 of 64, 1280 x 1280, 67 (17; 11 and 18),
+// 32768 of 4096, 128 x 128, 4360 (41; 59 and 97).
 static bool mx_experts_rows(long M, int experts) { return M <= 8L * experts || M <= 32; }
 
 size_t mx_experts_workspace_bytes(long M, long N, long K, int experts) {

@@ -153,7 +153,9 @@ int launch_mx_few_rows(const MxGemm& g, bool gated, const void* x, long ldx, hip
 
 // Whether one launch takes the product of a matrix: little work to quantise, or one slab.  us, one launch / quantised before it: 8 x 1280 x 10240 gated 5.5 / 7.9,
 // 32 x 2048 x 2560 gated 6.9 / 8.3, 32 x 1280 x 10240 gated 7.2 / 7.9; 8 x 5120 x 20480 19.5 / 16.4, 16 x 8192 x 2048 12.2 / 9.2.  (Against every wave quantising for
-// itself: 8 x 1280 x 5120 4.8 / 5.7, 3 x 6944 x 256 gated 8.2 / 16.8, 1 x 320 x 1280 3.5 / 3.2.)
+// itself: 8 x 1280 x 5120 4.8 / 5.7, 3 x 6944 x 256 gated 8.2 / 16.8, 1 x 320 x 1280 3.5 / 3.2.)  Linears without an activation have the kernel in which every wave does: it is
+// ahead with short reductions, 1 x 320 x 1280 3.0 where this one, without an activation, takes 3.4, 16 x 320 x 320 3.2 / 4.3, 32 x 640 x 640 4.1 / 5.4, and behind with others, 8 x 1280 x
+// 1280 4.4 / 3.9, 8 x 1280 x 5120 4.5 / 4.0, 24 x 2048 x 1280 5.9 / 5.1, 2 x 6944 x 256 9.1 / 6.2.
 bool mx_few_rows_takes(int M, int N, int K) { return M <= 32 && (K <= 2048 || mx_rows_quantizes(M, N, K)); }
 
 }  // namespace mq
